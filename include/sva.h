@@ -203,6 +203,40 @@ sva_status sva_rope_kv_write_qknorm(sva_cache* c, const sva_node* nodes, int32_t
                                     const float* gamma_k, const float* gamma_q, float eps,
                                     sva_stream s);
 
+/* Token rows where they lie: token t of a call (node t / T, token t % T) is the
+ * [H][d] bf16 elements at data + t * token_stride.  token_stride counts elements:
+ * H*d for a dense [n_nodes][T][H][d] tensor, 3*H*d for the q, k or v part of
+ * [n_nodes][T][3][H][d].  data 16-byte aligned, token_stride >= H*d and a multiple
+ * of 8. */
+typedef struct {
+  const void* data;
+  int64_t token_stride;
+} sva_token_rows;
+
+/* sva_rope_kv_write with an RMS normalisation of each head's key (and query) in
+ * front of the rotation, in one pass (reading: the paper names no normalisation;
+ * most DiTs that normalise q and k do it per head).  For a row x of d elements of
+ * one token and head:
+ *   x' = x * gamma / sqrt(mean(x^2) + eps),
+ * then RoPE; V is copied unchanged.  fp32 arithmetic, one bf16 rounding of the
+ * rotated result.
+ *   k, v, q   the nodes' new keys, values and queries; q may be NULL
+ *   q_out     [n_nodes][T][H][d] bf16, receives Q'; given exactly where q is.  May
+ *             be q's own data when q is dense; otherwise shares no memory with k,
+ *             v or q
+ *   gamma_k, gamma_q  fp32 device vectors of gamma_heads * d elements, 16-byte
+ *             aligned: one vector for all heads (gamma_heads = 1) or one a head
+ *             (gamma_heads = H); both NULL: all ones.  gamma_q is not read without q
+ *   eps       finite and > 0
+ * A chunk may be as short as one token.  Marks the own slots resident.
+ * Stream-ordered.  Errors: as sva_rope_kv_write, plus INVALID_ARGUMENT for bad
+ * strides, gammas, eps or an overlapping q_out. */
+sva_status sva_rope_kv_write_headnorm(sva_cache* c, const sva_node* nodes, int32_t n_nodes,
+                                      const sva_token_rows* k, const sva_token_rows* v,
+                                      const sva_token_rows* q, void* q_out, const float* gamma_k,
+                                      const float* gamma_q, int32_t gamma_heads, float eps,
+                                      sva_stream s);
+
 /* The linear projection in front of the attention layer, producing the
  * token-major inputs of sva_rope_kv_write (the paper's denoiser is a DiT
  * whose attention layers take q, k, v from the token features; Section 3.2

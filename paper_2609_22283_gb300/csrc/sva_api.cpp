@@ -257,6 +257,29 @@ sva_status check_own(const sva_cache* c, const sva_node& n, int i, bool need_res
   return SVA_OK;
 }
 
+// The checks of the nodes whose own slots a launch writes: bound, distinct,
+// positions inside the RoPE table.  Fills the kernel's node list.
+sva_status check_written(const sva_cache* c, const sva_node* nodes, int n_nodes, sva::RopeNode* out) {
+  const sva_geometry& g = c->g;
+  for (int i = 0; i < n_nodes; ++i) {
+    const sva_node& n = nodes[i];
+    sva_status st = check_own(c, n, i, false);
+    if (st != SVA_OK) return st;
+    for (int k = 0; k < i; ++k)
+      if (nodes[k].own_slot == n.own_slot)
+        return fail(SVA_ERR_INVALID_ARGUMENT, "nodes %d and %d write the same slot %d", k, i,
+                    n.own_slot);
+    const long long t0 = (long long)g.frames * n.chunk;
+    if (t0 < 0 || t0 + g.frames > g.max_frames)
+      return fail(SVA_ERR_CAPACITY,
+                  "node %d: chunk %d covers frames [%lld, %lld), outside the RoPE table [0, %d)", i,
+                  n.chunk, t0, t0 + g.frames, g.max_frames);
+    out[i].slot = n.own_slot;
+    out[i].t_base = (int32_t)t0;
+  }
+  return SVA_OK;
+}
+
 // Split workspace: room for 4 waves of split work items (one per SM and
 // wave), each 256 query rows x (d + 2) fp32, after one arrival counter per
 // item.
@@ -626,22 +649,8 @@ sva_status rope_write(sva_cache* c, const sva_node* nodes, int32_t n_nodes, cons
   if (st != SVA_OK) return st;
   const sva_geometry& g = c->g;
   sva::RopeParams p{};
-  for (int i = 0; i < n_nodes; ++i) {
-    const sva_node& n = nodes[i];
-    st = check_own(c, n, i, false);
-    if (st != SVA_OK) return st;
-    for (int k = 0; k < i; ++k)
-      if (nodes[k].own_slot == n.own_slot)
-        return fail(SVA_ERR_INVALID_ARGUMENT, "nodes %d and %d write the same slot %d", k, i,
-                    n.own_slot);
-    const long long t0 = (long long)g.frames * n.chunk;
-    if (t0 < 0 || t0 + g.frames > g.max_frames)
-      return fail(SVA_ERR_CAPACITY,
-                  "node %d: chunk %d covers frames [%lld, %lld), outside the RoPE table [0, %d)", i,
-                  n.chunk, t0, t0 + g.frames, g.max_frames);
-    p.nodes[i].slot = n.own_slot;
-    p.nodes[i].t_base = (int32_t)t0;
-  }
+  st = check_written(c, nodes, n_nodes, p.nodes);
+  if (st != SVA_OK) return st;
   p.k_new = k_new;
   p.v_new = v_new;
   p.q = q_inout;
@@ -691,6 +700,94 @@ sva_status sva_rope_kv_write_qknorm(sva_cache* c, const sva_node* nodes, int32_t
   if (!std::isfinite(eps) || !(eps > 0.0f))
     return fail(SVA_ERR_INVALID_ARGUMENT, "eps must be finite and > 0");
   return rope_write(c, nodes, n_nodes, k_new, v_new, q_inout, gamma_k, gamma_q, eps, s);
+}
+
+sva_status sva_rope_kv_write_headnorm(sva_cache* c, const sva_node* nodes, int32_t n_nodes,
+                                      const sva_token_rows* k, const sva_token_rows* v,
+                                      const sva_token_rows* q, void* q_out, const float* gamma_k,
+                                      const float* gamma_q, int32_t gamma_heads, float eps,
+                                      sva_stream s) {
+  if (c == nullptr || nodes == nullptr || k == nullptr || v == nullptr)
+    return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  if (n_nodes < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_nodes %d < 1", n_nodes);
+  if (n_nodes > SVA_MAX_NODES)
+    return fail(SVA_ERR_CAPACITY, "n_nodes %d > SVA_MAX_NODES (%d)", n_nodes, SVA_MAX_NODES);
+  const sva_geometry& g = c->g;
+  const int64_t row = (int64_t)g.num_heads * g.head_dim;
+  const int64_t tokens = (int64_t)n_nodes * c->L.T;
+  const bool has_q = q != nullptr;
+  if (has_q != (q_out != nullptr))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "q and q_out come together or not at all");
+  const sva_token_rows* in[3] = {k, v, q};
+  const char* names[3] = {"k", "v", "q"};
+  for (int i = 0; i < (has_q ? 3 : 2); ++i) {
+    if (in[i]->data == nullptr || !aligned16(in[i]->data))
+      return fail(SVA_ERR_INVALID_ARGUMENT, "%s must be non-NULL and 16-byte aligned", names[i]);
+    if (in[i]->token_stride < row || in[i]->token_stride % 8 != 0 || in[i]->token_stride > (1ll << 40))
+      return fail(SVA_ERR_INVALID_ARGUMENT,
+                  "%s: token stride %lld must be a multiple of 8 elements and >= H*d = %lld", names[i],
+                  (long long)in[i]->token_stride, (long long)row);
+  }
+  if (has_q) {
+    if (!aligned16(q_out)) return fail(SVA_ERR_INVALID_ARGUMENT, "q_out must be 16-byte aligned");
+    // q_out is written while other tokens are still read: apart from q itself,
+    // token on token, it may share no memory with an input
+    const uintptr_t o0 = reinterpret_cast<uintptr_t>(q_out), o1 = o0 + (uintptr_t)(tokens * row * 2);
+    for (int i = 0; i < 3; ++i) {
+      const uintptr_t i0 = reinterpret_cast<uintptr_t>(in[i]->data);
+      const uintptr_t i1 = i0 + (uintptr_t)(((tokens - 1) * in[i]->token_stride + row) * 2);
+      if (i == 2 && i0 == o0 && in[i]->token_stride == row) continue;
+      if (i0 < o1 && o0 < i1)
+        return fail(SVA_ERR_INVALID_ARGUMENT,
+                    "q_out overlaps %s (only q itself, with dense tokens, may be rotated in place)", names[i]);
+    }
+  }
+  if (gamma_heads != 1 && gamma_heads != g.num_heads)
+    return fail(SVA_ERR_INVALID_ARGUMENT, "gamma_heads %d is neither 1 nor num_heads = %d", gamma_heads,
+                g.num_heads);
+  if (!aligned16(gamma_k) || !aligned16(gamma_q) || (has_q && (gamma_k == nullptr) != (gamma_q == nullptr)))
+    return fail(SVA_ERR_INVALID_ARGUMENT,
+                "gamma_k and gamma_q must be 16-byte aligned, with q both given or both NULL");
+  if (!std::isfinite(eps) || !(eps > 0.0f))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "eps must be finite and > 0");
+  sva_status st = check_device(c);
+  if (st != SVA_OK) return st;
+  sva::RopeHeadParams p{};
+  st = check_written(c, nodes, n_nodes, p.nodes);
+  if (st != SVA_OK) return st;
+  p.k = k->data;
+  p.v = v->data;
+  p.k_stride = k->token_stride;
+  p.v_stride = v->token_stride;
+  if (has_q) {
+    p.q = q->data;
+    p.q_stride = q->token_stride;
+    p.q_out = q_out;
+  }
+  p.cache = c->base;
+  p.tab_t = reinterpret_cast<const float2*>(c->base + c->L.tab_t);
+  p.tab_h = reinterpret_cast<const float2*>(c->base + c->L.tab_h);
+  p.tab_w = reinterpret_cast<const float2*>(c->base + c->L.tab_w);
+  p.gamma_k = gamma_k;
+  p.gamma_q = has_q ? gamma_q : nullptr;
+  p.gamma = gamma_k == nullptr ? sva::HeadGamma::kNone
+            : gamma_heads == 1 ? sva::HeadGamma::kShared
+                               : sva::HeadGamma::kHeads;
+  p.eps = eps;
+  p.T = c->L.T;
+  p.H = g.num_heads;
+  p.d = g.head_dim;
+  p.Tpad = c->L.Tpad;
+  p.Hp = g.grid_h;
+  p.Wp = g.grid_w;
+  p.P0 = g.rope_pairs[0];
+  p.P1 = g.rope_pairs[1];
+  p.P2 = g.rope_pairs[2];
+  p.n_nodes = n_nodes;
+  cudaError_t e = sva::launch_rope_head(p, c->num_sms, reinterpret_cast<cudaStream_t>(s));
+  if (e != cudaSuccess) return cuda_fail(e, "rope_head launch");
+  for (int i = 0; i < n_nodes; ++i) c->slots[nodes[i].own_slot].resident = true;
+  return ok();
 }
 
 }  // extern "C"
@@ -1064,23 +1161,8 @@ sva_status project(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const v
     }
   }
   if (rope) {
-    // the same node checks as sva_rope_kv_write
-    for (int i = 0; i < n_nodes; ++i) {
-      const sva_node& n = nodes[i];
-      st = check_own(c, n, i, false);
-      if (st != SVA_OK) return st;
-      for (int j = 0; j < i; ++j)
-        if (nodes[j].own_slot == n.own_slot)
-          return fail(SVA_ERR_INVALID_ARGUMENT, "nodes %d and %d write the same slot %d", j, i,
-                      n.own_slot);
-      const long long t0 = (long long)g.frames * n.chunk;
-      if (t0 < 0 || t0 + g.frames > g.max_frames)
-        return fail(SVA_ERR_CAPACITY,
-                    "node %d: chunk %d covers frames [%lld, %lld), outside the RoPE table [0, %d)",
-                    i, n.chunk, t0, t0 + g.frames, g.max_frames);
-      p.rope.nodes[i].slot = n.own_slot;
-      p.rope.nodes[i].t_base = (int32_t)t0;
-    }
+    st = check_written(c, nodes, n_nodes, p.rope.nodes);
+    if (st != SVA_OK) return st;
     p.rope_on = 1;
     p.rope.cache = c->base;
     p.rope.tab_t = reinterpret_cast<const float2*>(c->base + c->L.tab_t);

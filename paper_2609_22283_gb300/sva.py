@@ -37,7 +37,8 @@ MAX_NODES = 64
 
 EXPORTED = ("sva_cache_bytes", "sva_cache_create", "sva_cache_bind", "sva_cache_lookup",
             "sva_cache_release", "sva_select_context", "sva_pipeline_round", "sva_check_pipeline",
-            "sva_rope_kv_write", "sva_rope_kv_write_qknorm", "sva_attend_nodes",
+            "sva_rope_kv_write", "sva_rope_kv_write_qknorm", "sva_rope_kv_write_headnorm",
+            "sva_attend_nodes",
             "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_qkv_project",
             "sva_qkv_project_rope",
             "sva_attend_workspace_bytes",
@@ -65,6 +66,10 @@ class sva_node(ctypes.Structure):
                 ("ctx_slot", ctypes.c_int32 * MAX_CTX), ("ctx_visible", ctypes.c_uint8 * MAX_CTX)]
 
 
+class sva_token_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64)]
+
+
 class sva_attn_mask(ctypes.Structure):
     _fields_ = [("tile_mask", ctypes.c_void_p), ("tile_words", ctypes.c_int32),
                 ("own_mask", ctypes.c_void_p), ("own_words", ctypes.c_int32),
@@ -87,6 +92,7 @@ def load(path: str = LIB_PATH):
     i32, p, pi32 = ctypes.c_int32, ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32)
     pg = ctypes.POINTER(sva_geometry)
     pn = ctypes.POINTER(sva_node)
+    pr = ctypes.POINTER(sva_token_rows)
     sig = {
         "sva_cache_bytes": ([pg], ctypes.c_size_t),
         "sva_cache_create": ([pg, p, ctypes.c_size_t, ctypes.POINTER(p)], i32),
@@ -98,6 +104,7 @@ def load(path: str = LIB_PATH):
         "sva_check_pipeline": ([i32, i32, i32, i32, pi32, pi32], i32),
         "sva_rope_kv_write": ([p, pn, i32, p, p, p, p], i32),
         "sva_rope_kv_write_qknorm": ([p, pn, i32, p, p, p, p, p, ctypes.c_float, p], i32),
+        "sva_rope_kv_write_headnorm": ([p, pn, i32, pr, pr, pr, p, p, p, i32, ctypes.c_float, p], i32),
         "sva_attend_nodes": ([p, pn, i32, p, p, p, ctypes.c_float, p], i32),
         "sva_attend_nodes_sparse": ([p, pn, i32, p, p, p, ctypes.c_float, p, i32, p], i32),
         "sva_qkv_project": ([p, p, i32, i32, p, p, p, p, p, p], i32),
@@ -142,6 +149,22 @@ def _tok_major(t: torch.Tensor, name: str, n: int, T: int, H: int, d: int):
         raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor")
     if t.shape != (n, T, H, d):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, T, H, d)}")
+
+
+def _token_rows(t: torch.Tensor, name: str, n: int, T: int, H: int, d: int) -> sva_token_rows:
+    """A bf16 [n][T][H][d] tensor whose tokens lie at one stride, each dense: a tensor of its own, or the
+    q, k or v part of a packed one."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name} must be a bf16 CUDA tensor")
+    if t.shape != (n, T, H, d):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, T, H, d)}")
+    node, tok, head, one = t.stride()
+    if T == 1:  # the stride of a dimension of one element says nothing: the nodes are the tokens
+        tok = node if n > 1 else H * d
+    if (one != 1 or (H > 1 and head != d) or (n > 1 and node != T * tok)
+            or (tok < H * d and n * T > 1)):
+        raise ValueError(f"{name} must hold dense [H][d] rows at one token stride (strides {t.stride()})")
+    return sva_token_rows(t.data_ptr(), max(tok, H * d))
 
 
 # ---------------------------------------------------------------- selection (host)
@@ -289,6 +312,39 @@ class Cache:
             gamma_q.data_ptr() if gamma_q is not None else None, float(eps),
             _stream_handle(stream))
         _check(st)
+
+    def rope_kv_write_headnorm(self, nodes, k_new, v_new, q=None, q_out=None, gamma_k=None,
+                               gamma_q=None, eps=1e-6, stream=None):
+        """sva_rope_kv_write_headnorm: RMSNorm of each head (fp32 gammas [d] or [H][d], or None),
+        RoPE and the cache write.  k_new, v_new, q: bf16 [n][T][H][d], dense or parts of a packed
+        tensor; q_out: dense, receives Q' (None: q itself, which then is dense)."""
+        arr, count = _node_array(nodes)
+        rk = _token_rows(k_new, "k_new", count, self.T, self.H, self.d)
+        rv = _token_rows(v_new, "v_new", count, self.T, self.H, self.d)
+        rq = None
+        if q is not None:
+            rq = _token_rows(q, "q", count, self.T, self.H, self.d)
+            q_out = q if q_out is None else q_out
+            _tok_major(q_out, "q_out", count, self.T, self.H, self.d)
+        elif q_out is not None or gamma_q is not None:
+            raise ValueError("q_out and gamma_q are for calls with q")
+        heads = 1
+        for gm, nm in ((gamma_k, "gamma_k"), (gamma_q, "gamma_q")):
+            if gm is None:
+                continue
+            if gm.dtype != torch.float32 or not gm.is_cuda or not gm.is_contiguous():
+                raise ValueError(f"{nm} must be a contiguous fp32 CUDA tensor")
+            if gm.shape not in ((self.d,), (self.H, self.d)):
+                raise ValueError(f"{nm} has shape {tuple(gm.shape)}, expected [{self.d}] or [{self.H}][{self.d}]")
+            heads = self.H if gm.dim() == 2 else 1
+        if gamma_k is not None and gamma_q is not None and gamma_k.shape != gamma_q.shape:
+            raise ValueError("gamma_k and gamma_q must have the same shape")
+        _check(_lib.sva_rope_kv_write_headnorm(
+            self.handle, arr, count, ctypes.byref(rk), ctypes.byref(rv),
+            ctypes.byref(rq) if rq is not None else None, q_out.data_ptr() if rq is not None else None,
+            gamma_k.data_ptr() if gamma_k is not None else None,
+            gamma_q.data_ptr() if gamma_q is not None else None, heads, float(eps),
+            _stream_handle(stream)))
 
     def attend_nodes(self, nodes, q, out, lse=None, scale=None, stream=None, check=True):
         arr, count = _node_array(nodes)
