@@ -360,6 +360,30 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
                                    const void* q, void* out, float* lse, float scale,
                                    const sva_attn_mask* mask, sva_stream s);
 
+/* How much attention every key got: the column sums of the softmax weights of an
+ * attention launch, for the slots its nodes see (the own ones included).  For slot
+ * s, head h and key token v:
+ *   out[s][h][v] = decay * prev[s][h][v]
+ *                  + sum_i sum_u exp(scale * q[i][u][h] . k_v + M(u, v) - lse[i][h][u])
+ * over the nodes i that see s and their queries u, with M the mask of the
+ * attention launch (hidden context slots, the within-chunk mode and `mask`).  A
+ * query whose lse is -inf saw no key and adds nothing.  Accumulated from round to
+ * round this says which tokens of the history are still read (sva_cache_condense).
+ *   q      [n_nodes][T][H][d] bf16, the (rotated) queries of the attention launch
+ *   lse    [n_nodes][H][T] fp32, what that launch returned
+ *   scale  its logit scale
+ *   mask   its masks, or NULL
+ *   prev   [num_slots][H][T] fp32, or NULL: nothing before (decay is then not used)
+ *   decay  0..1
+ *   out    [num_slots][H][T] fp32; only the slots that some node sees are written.
+ *          May be prev itself, otherwise shares no memory with it
+ * fp32 throughout (the products of bf16 accumulate in fp32); the same inputs give
+ * the same bits.  Stream-ordered.  Errors: as sva_attend_nodes_masked, plus
+ * INVALID_ARGUMENT for decay. */
+sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
+                              const float* lse, float scale, const sva_attn_mask* mask,
+                              const float* prev, float decay, float* out, sva_stream s);
+
 /* Bytes of the optional split workspace of a cache (0 if c is NULL).  With
  * a workspace attached, sva_attend_nodes may divide each (node, head,
  * query-tile pair) work unit into contiguous key ranges (up to 4, or up to 8
@@ -425,7 +449,8 @@ sva_status sva_poll_device_status(sva_cache* c, sva_stream s);
  * own copies and MMAs in flight, frees its tensor memory and exits, and
  * sva_poll_device_status reports the timeout.  Needs nodes of >= 2 key
  * tiles.  mode 0 clears the hook.  timeout_s (1 ms .. 60 s) also becomes the
- * bounded-wait limit of this cache's later launches (default 1 s).
+ * bounded-wait limit of this cache's later launches (default 1 s).  mode 2 does
+ * the same to the second Q tile of every CTA of the next sva_attend_weights.
  * Errors: INVALID_ARGUMENT. */
 sva_status sva_debug_inject(sva_cache* c, int32_t mode, double timeout_s);
 

@@ -23,6 +23,7 @@
 #include "internal.h"
 #include "proj.h"
 #include "sva.h"
+#include "weights.h"
 
 namespace {
 
@@ -152,6 +153,7 @@ struct SlotInfo {
   bool bound = false;
   bool resident = false;
   int32_t seq = 0, chunk = 0, level = 0;
+  int32_t listed = -1;  // scratch of a call: its place in the call's list of slots, -1 between calls
 };
 
 using StateKey = std::tuple<int32_t, int32_t, int32_t>;
@@ -276,6 +278,92 @@ sva_status check_written(const sva_cache* c, const sva_node* nodes, int n_nodes,
                   n.chunk, t0, t0 + g.frames, g.max_frames);
     out[i].slot = n.own_slot;
     out[i].t_base = (int32_t)t0;
+  }
+  return SVA_OK;
+}
+
+// The checks of the states that nodes read, and each node's list of the slots
+// it sees (own first, then the visible contexts).
+sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sva::AttnNode* out) {
+  const sva_geometry& g = c->g;
+  for (int i = 0; i < n_nodes; ++i) {
+    const sva_node& n = nodes[i];
+    sva_status st = check_own(c, n, i, true);
+    if (st != SVA_OK) return st;
+    if (n.n_ctx < 0 || n.n_ctx > SVA_MAX_CTX)
+      return fail(SVA_ERR_CAPACITY, "node %d: n_ctx %d outside 0..%d", i, n.n_ctx, SVA_MAX_CTX);
+    if (n.within != SVA_WITHIN_BIDIRECTIONAL && n.within != SVA_WITHIN_FRAME_CAUSAL)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: unknown within-chunk mode %d", i, n.within);
+    sva::AttnNode& a = out[i];
+    a.q_index = i;
+    a.frame_causal = n.within == SVA_WITHIN_FRAME_CAUSAL ? 1 : 0;
+    a.slot[0] = n.own_slot;
+    a.src[0] = 0;
+    int nkv = 1;
+    for (int k = 0; k < n.n_ctx; ++k) {
+      const int32_t cs = n.ctx_slot[k];
+      if (cs < 0 || cs >= g.num_slots)
+        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d: slot %d out of range", i, k, cs);
+      const SlotInfo& si = c->slots[cs];
+      if (!si.bound || !si.resident)
+        return fail(SVA_ERR_NOT_RESIDENT, "node %d ctx %d: slot %d is %s", i, k, cs,
+                    si.bound ? "bound but not written" : "not bound");
+      if (si.seq != n.seq || si.chunk >= n.chunk)
+        return fail(SVA_ERR_CAUSALITY,
+                    "node %d (seq %d, chunk %d) ctx %d: slot %d holds (seq %d, chunk %d), not a "
+                    "past chunk of the same sequence",
+                    i, n.seq, n.chunk, k, cs, si.seq, si.chunk);
+      if (cs == n.own_slot)
+        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d repeats the own slot", i, k);
+      for (int k2 = 0; k2 < k; ++k2)
+        if (n.ctx_slot[k2] == cs)
+          return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: slot %d listed twice", i, cs);
+      if (n.ctx_visible[k]) {
+        a.src[nkv] = (uint8_t)(1 + k);
+        a.slot[nkv++] = cs;
+      }
+    }
+    a.n_kv = nkv;
+  }
+  return SVA_OK;
+}
+
+// The checks of a launch's masks.
+sva_status check_masks(const sva_cache* c, const sva_node* nodes, int n_nodes, const sva_attn_mask& m) {
+  const int nt_slot = c->L.Tpad / sva::kTile;
+  if (m.tile_mask != nullptr) {
+    if ((reinterpret_cast<uintptr_t>(m.tile_mask) & 3u) != 0)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "tile_mask must be 4-byte aligned");
+    for (int i = 0; i < n_nodes; ++i) {
+      const long long bits = (long long)(1 + nodes[i].n_ctx) * nt_slot;
+      if (bits > 32LL * sva::kMaskWords)
+        return fail(SVA_ERR_CAPACITY, "node %d: %lld key tiles exceed the %d a tile mask covers",
+                    i, bits, 32 * sva::kMaskWords);
+      if (m.tile_words < (bits + 31) / 32)
+        return fail(SVA_ERR_INVALID_ARGUMENT,
+                    "node %d: words_per_row %d < %lld needed for %lld key tiles", i, m.tile_words,
+                    (bits + 31) / 32, bits);
+    }
+  }
+  if (m.own_mask != nullptr) {
+    if ((reinterpret_cast<uintptr_t>(m.own_mask) & 3u) != 0)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "own_mask must be 4-byte aligned");
+    if (m.own_words < (c->L.T + 31) / 32)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "own_words %d < %d needed for %d tokens", m.own_words,
+                  (c->L.T + 31) / 32, c->L.T);
+  }
+  if (m.hist_mask != nullptr) {
+    if ((reinterpret_cast<uintptr_t>(m.hist_mask) & 3u) != 0)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_mask must be 4-byte aligned");
+    if (m.hist_words < (c->L.T + 31) / 32)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_words %d < %d needed for %d tokens", m.hist_words,
+                  (c->L.T + 31) / 32, c->L.T);
+    if (m.hist_states < 1)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_states %d < 1", m.hist_states);
+    for (int i = 0; i < n_nodes; ++i)
+      if (nodes[i].n_ctx > m.hist_states)
+        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d has %d context states, hist_states is %d",
+                    i, nodes[i].n_ctx, m.hist_states);
   }
   return SVA_OK;
 }
@@ -801,13 +889,10 @@ enum class Scratch {
 };
 
 // sva_attend_nodes, _sparse, _masked and _noalloc: the checks, the launch
-// parameters, the split plan and the launch.  tile_mask, own_mask and
-// hist_mask NULL is
-// the dense mask.  Every check runs before anything is enqueued.
+// parameters, the split plan and the launch.  A mask of NULLs is the dense mask.
+// Every check runs before anything is enqueued.
 sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q, void* out,
-                  float* lse, float scale, const uint32_t* tile_mask, int32_t mask_words,
-                  const uint32_t* own_mask, int32_t own_words, const uint32_t* hist_mask,
-                  int32_t hist_states, int32_t hist_words, sva_stream s, Scratch scratch) {
+                  float* lse, float scale, const sva_attn_mask& mask, sva_stream s, Scratch scratch) {
   if (c == nullptr || nodes == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
   if (n_nodes < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_nodes %d < 1", n_nodes);
   if (n_nodes > SVA_MAX_NODES)
@@ -823,89 +908,20 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
 
   static thread_local sva::AttnParams p;  // ~5 KB: kept off the stack
   std::memset(&p, 0, sizeof(p));
-  for (int i = 0; i < n_nodes; ++i) {
-    const sva_node& n = nodes[i];
-    st = check_own(c, n, i, true);
-    if (st != SVA_OK) return st;
-    if (n.n_ctx < 0 || n.n_ctx > SVA_MAX_CTX)
-      return fail(SVA_ERR_CAPACITY, "node %d: n_ctx %d outside 0..%d", i, n.n_ctx, SVA_MAX_CTX);
-    if (n.within != SVA_WITHIN_BIDIRECTIONAL && n.within != SVA_WITHIN_FRAME_CAUSAL)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: unknown within-chunk mode %d", i, n.within);
-    sva::AttnNode& a = p.nodes[i];
-    a.q_index = i;
-    a.frame_causal = n.within == SVA_WITHIN_FRAME_CAUSAL ? 1 : 0;
-    a.slot[0] = n.own_slot;
-    a.src[0] = 0;
-    int nkv = 1;
-    for (int k = 0; k < n.n_ctx; ++k) {
-      const int32_t cs = n.ctx_slot[k];
-      if (cs < 0 || cs >= g.num_slots)
-        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d: slot %d out of range", i, k, cs);
-      const SlotInfo& si = c->slots[cs];
-      if (!si.bound || !si.resident)
-        return fail(SVA_ERR_NOT_RESIDENT, "node %d ctx %d: slot %d is %s", i, k, cs,
-                    si.bound ? "bound but not written" : "not bound");
-      if (si.seq != n.seq || si.chunk >= n.chunk)
-        return fail(SVA_ERR_CAUSALITY,
-                    "node %d (seq %d, chunk %d) ctx %d: slot %d holds (seq %d, chunk %d), not a "
-                    "past chunk of the same sequence",
-                    i, n.seq, n.chunk, k, cs, si.seq, si.chunk);
-      if (cs == n.own_slot)
-        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d repeats the own slot", i, k);
-      for (int k2 = 0; k2 < k; ++k2)
-        if (n.ctx_slot[k2] == cs)
-          return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: slot %d listed twice", i, cs);
-      if (n.ctx_visible[k]) {
-        a.src[nkv] = (uint8_t)(1 + k);
-        a.slot[nkv++] = cs;
-      }
-    }
-    a.n_kv = nkv;
-  }
+  st = check_read(c, nodes, n_nodes, p.nodes);
+  if (st != SVA_OK) return st;
   p.n_qt = (c->L.T + sva::kTile - 1) / sva::kTile;
   p.nt_slot = c->L.Tpad / sva::kTile;
-  if (tile_mask != nullptr) {
-    if ((reinterpret_cast<uintptr_t>(tile_mask) & 3u) != 0)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "tile_mask must be 4-byte aligned");
-    for (int i = 0; i < n_nodes; ++i) {
-      const long long bits = (long long)(1 + nodes[i].n_ctx) * p.nt_slot;
-      if (bits > 32LL * sva::kMaskWords)
-        return fail(SVA_ERR_CAPACITY, "node %d: %lld key tiles exceed the %d a tile mask covers",
-                    i, bits, 32 * sva::kMaskWords);
-      if (mask_words < (bits + 31) / 32)
-        return fail(SVA_ERR_INVALID_ARGUMENT,
-                    "node %d: words_per_row %d < %lld needed for %lld key tiles", i, mask_words,
-                    (bits + 31) / 32, bits);
-    }
-    p.tile_mask = tile_mask;
-    p.mask_words = mask_words;
-  }
-  if (own_mask != nullptr) {
-    if ((reinterpret_cast<uintptr_t>(own_mask) & 3u) != 0)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "own_mask must be 4-byte aligned");
-    if (own_words < (c->L.T + 31) / 32)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "own_words %d < %d needed for %d tokens", own_words,
-                  (c->L.T + 31) / 32, c->L.T);
-    p.own_mask = own_mask;
-    p.own_words = own_words;
-  }
-  if (hist_mask != nullptr) {
-    if ((reinterpret_cast<uintptr_t>(hist_mask) & 3u) != 0)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_mask must be 4-byte aligned");
-    if (hist_words < (c->L.T + 31) / 32)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_words %d < %d needed for %d tokens", hist_words,
-                  (c->L.T + 31) / 32, c->L.T);
-    if (hist_states < 1)
-      return fail(SVA_ERR_INVALID_ARGUMENT, "hist_states %d < 1", hist_states);
-    for (int i = 0; i < n_nodes; ++i)
-      if (nodes[i].n_ctx > hist_states)
-        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d has %d context states, hist_states is %d",
-                    i, nodes[i].n_ctx, hist_states);
-    p.hist_mask = hist_mask;
-    p.hist_states = hist_states;
-    p.hist_words = hist_words;
-  }
-  p.masked = (tile_mask != nullptr || own_mask != nullptr || hist_mask != nullptr) ? 1 : 0;
+  st = check_masks(c, nodes, n_nodes, mask);
+  if (st != SVA_OK) return st;
+  p.tile_mask = mask.tile_mask;
+  p.mask_words = mask.tile_words;
+  p.own_mask = mask.own_mask;
+  p.own_words = mask.own_words;
+  p.hist_mask = mask.hist_mask;
+  p.hist_states = mask.hist_states;
+  p.hist_words = mask.hist_words;
+  p.masked = (p.tile_mask != nullptr || p.own_mask != nullptr || p.hist_mask != nullptr) ? 1 : 0;
   if (p.masked)  // the masked kernel keeps a bitmap of the node's key tiles
     for (int i = 0; i < n_nodes; ++i)
       if ((long long)p.nodes[i].n_kv * p.nt_slot > 32LL * sva::kMaskWords)
@@ -1014,9 +1030,9 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
   p.n_nodes = n_nodes;
   p.valid_last = c->L.T - (p.nt_slot - 1) * sva::kTile;
   p.frame_tokens = g.grid_h * g.grid_w;
-  p.fault_mode = scratch == Scratch::kStatic ? 0 : c->fault_mode;
+  p.fault_mode = scratch != Scratch::kStatic && c->fault_mode == 1 ? 1 : 0;
   p.timeout_ns = c->timeout_ns;
-  if (scratch != Scratch::kStatic) c->fault_mode = 0;
+  if (p.fault_mode != 0) c->fault_mode = 0;
   p.n_full = (int32_t)n_full;
   p.n_split = n_split;
   p.cluster = plan.cluster ? 1 : 0;
@@ -1061,8 +1077,7 @@ extern "C" {
 
 sva_status sva_attend_nodes(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
                             void* out, float* lse, float scale, sva_stream s) {
-  return attend(c, nodes, n_nodes, q, out, lse, scale, nullptr, 0, nullptr, 0, nullptr, 0, 0, s,
-                Scratch::kWorkspace);
+  return attend(c, nodes, n_nodes, q, out, lse, scale, sva_attn_mask{}, s, Scratch::kWorkspace);
 }
 
 }  // extern "C"
@@ -1241,19 +1256,17 @@ sva_status sva_attend_nodes_sparse(sva_cache* c, const sva_node* nodes, int32_t 
                                    const uint32_t* tile_mask, int32_t words_per_row,
                                    sva_stream s) {
   if (tile_mask == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "tile_mask is NULL");
-  return attend(c, nodes, n_nodes, q, out, lse, scale, tile_mask, words_per_row, nullptr, 0,
-                nullptr, 0, 0, s, Scratch::kWorkspace);
+  sva_attn_mask mask{};
+  mask.tile_mask = tile_mask;
+  mask.tile_words = words_per_row;
+  return attend(c, nodes, n_nodes, q, out, lse, scale, mask, s, Scratch::kWorkspace);
 }
 
 sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t n_nodes,
                                    const void* q, void* out, float* lse, float scale,
                                    const sva_attn_mask* mask, sva_stream s) {
-  if (mask == nullptr)
-    return attend(c, nodes, n_nodes, q, out, lse, scale, nullptr, 0, nullptr, 0, nullptr, 0, 0, s,
-                  Scratch::kWorkspace);
-  return attend(c, nodes, n_nodes, q, out, lse, scale, mask->tile_mask, mask->tile_words,
-                mask->own_mask, mask->own_words, mask->hist_mask, mask->hist_states,
-                mask->hist_words, s, Scratch::kWorkspace);
+  return attend(c, nodes, n_nodes, q, out, lse, scale, mask != nullptr ? *mask : sva_attn_mask{}, s,
+                Scratch::kWorkspace);
 }
 
 // Attention with the split scratch taken from the library's own device
@@ -1263,8 +1276,112 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
 sva_status sva_attend_nodes_noalloc(sva_cache* c, const sva_node* nodes, int32_t n_nodes,
                                     const void* q, void* out, float* lse, float scale,
                                     sva_stream s) {
-  return attend(c, nodes, n_nodes, q, out, lse, scale, nullptr, 0, nullptr, 0, nullptr, 0, 0, s,
-                Scratch::kStatic);
+  return attend(c, nodes, n_nodes, q, out, lse, scale, sva_attn_mask{}, s, Scratch::kStatic);
+}
+
+sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
+                              const float* lse, float scale, const sva_attn_mask* mask,
+                              const float* prev, float decay, float* out, sva_stream s) {
+  if (c == nullptr || nodes == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  if (n_nodes < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_nodes %d < 1", n_nodes);
+  if (n_nodes > SVA_MAX_NODES)
+    return fail(SVA_ERR_CAPACITY, "n_nodes %d > SVA_MAX_NODES (%d)", n_nodes, SVA_MAX_NODES);
+  auto aligned4 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 3u) == 0; };
+  if (q == nullptr || lse == nullptr || out == nullptr || !aligned16(q) || !aligned4(lse) ||
+      !aligned4(prev) || !aligned4(out))
+    return fail(SVA_ERR_INVALID_ARGUMENT,
+                "q, lse, out must be non-NULL, q 16-byte and lse, prev, out 4-byte aligned");
+  if (!std::isfinite(scale) || !(scale > 0.0f))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "scale must be finite and > 0");
+  if (!(decay >= 0.0f && decay <= 1.0f))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "decay must be in [0, 1]");
+  sva_status st = check_device(c);
+  if (st != SVA_OK) return st;
+  const sva_geometry& g = c->g;
+  static thread_local sva::AttnNode reads[SVA_MAX_NODES];
+  st = check_read(c, nodes, n_nodes, reads);
+  if (st != SVA_OK) return st;
+  const sva_attn_mask m = mask != nullptr ? *mask : sva_attn_mask{};
+  st = check_masks(c, nodes, n_nodes, m);
+  if (st != SVA_OK) return st;
+
+  static thread_local sva::WeightParams p;
+  std::memset(&p, 0, sizeof(p));
+  st = encode_4d_q(&p.tmap_q, q, g, c->L.T, n_nodes);
+  if (st != SVA_OK) return st;
+  p.tmap_kv = c->tmap_kv;
+  // The distinct slots and who sees them: count, order by that count, fill.
+  static thread_local int32_t slot[sva::kMaxWeightRefs], count[sva::kMaxWeightRefs];
+  int n_slots = 0;
+  p.masked = m.tile_mask != nullptr || m.own_mask != nullptr || m.hist_mask != nullptr ? 1 : 0;
+  for (int i = 0; i < n_nodes; ++i) {
+    if (reads[i].frame_causal) p.masked = 1;
+    for (int k = 0; k < reads[i].n_kv; ++k) {
+      int32_t& at = c->slots[reads[i].slot[k]].listed;
+      if (at < 0) {
+        at = n_slots;
+        slot[n_slots] = reads[i].slot[k];
+        count[n_slots++] = 0;
+      }
+      ++count[at];
+    }
+  }
+  int order = 0, refs = 0;
+  int32_t fewest = INT32_MAX;
+  for (int most = n_nodes; most >= 1; --most)
+    for (int i = 0; i < n_slots; ++i) {
+      if (count[i] != most) continue;
+      fewest = most;
+      p.slot[order] = slot[i];
+      p.first[order] = (uint16_t)refs;
+      refs += most;
+      c->slots[slot[i]].listed = order++;
+    }
+  p.first[n_slots] = (uint16_t)refs;
+  p.n_slots = n_slots;
+  std::memset(count, 0, sizeof(count[0]) * n_slots);
+  for (int i = 0; i < n_nodes; ++i)
+    for (int k = 0; k < reads[i].n_kv; ++k) {
+      const int at = c->slots[reads[i].slot[k]].listed;
+      p.ref[p.first[at] + count[at]++] =
+          (uint16_t)(i | reads[i].src[k] << sva::kRefStateShift |
+                     (k == 0 && reads[i].frame_causal ? sva::kRefCausal : 0));
+    }
+  for (int i = 0; i < n_slots; ++i) c->slots[slot[i]].listed = -1;
+
+  p.lse = lse;
+  p.prev = prev;
+  p.out = out;
+  p.decay = decay;
+  p.status = reinterpret_cast<int*>(c->base + c->L.status);
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.T = c->L.T;
+  p.Tpad = c->L.Tpad;
+  p.H = g.num_heads;
+  p.n_qt = c->L.Tpad / sva::kTile;
+  p.n_pairs = (p.n_qt + 1) / 2;
+  p.frame_tokens = g.grid_h * g.grid_w;
+  p.fault_mode = c->fault_mode == 2 ? 2 : 0;
+  if (p.fault_mode != 0) c->fault_mode = 0;
+  p.timeout_ns = c->timeout_ns;
+  p.tile_mask = m.tile_mask;
+  p.mask_words = m.tile_words;
+  p.own_mask = m.own_mask;
+  p.own_words = m.own_words;
+  p.hist_mask = m.hist_mask;
+  p.hist_states = m.hist_states;
+  p.hist_words = m.hist_words;
+  const long long units = (long long)n_slots * g.num_heads * p.n_pairs;  // < 2^23: the pool has < 2^31 rows
+  p.units = (int32_t)units;
+  // A unit whose SMs would otherwise idle is shared by a cluster, two Q tiles a
+  // CTA at least.
+  const long long tiles = (long long)fewest * p.n_qt;
+  p.n_split = (int32_t)std::max(1ll, std::min({(long long)sva::kMaxWeightSplit, c->num_sms / units, tiles / 2}));
+  long long grid = units * p.n_split;
+  if (!p.masked && p.n_split == 1) grid = std::min<long long>(units, c->num_sms);
+  cudaError_t e = sva::launch_weights(p, g.head_dim, (int)grid, reinterpret_cast<cudaStream_t>(s));
+  if (e != cudaSuccess) return cuda_fail(e, "attend_weights launch");
+  return ok();
 }
 
 sva_status sva_poll_device_status(sva_cache* c, sva_stream s) {
@@ -1324,7 +1441,7 @@ sva_status sva_cache_set_workspace(sva_cache* c, void* dev_buf, size_t bytes) {
 
 sva_status sva_debug_inject(sva_cache* c, int32_t mode, double timeout_s) {
   if (c == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
-  if (mode < 0 || mode > 1) return fail(SVA_ERR_INVALID_ARGUMENT, "unknown fault mode %d", mode);
+  if (mode < 0 || mode > 2) return fail(SVA_ERR_INVALID_ARGUMENT, "unknown fault mode %d", mode);
   if (!(timeout_s >= 1e-3 && timeout_s <= 60.0))
     return fail(SVA_ERR_INVALID_ARGUMENT, "timeout must be in [1 ms, 60 s]");
   c->fault_mode = mode;

@@ -39,7 +39,7 @@ EXPORTED = ("sva_cache_bytes", "sva_cache_create", "sva_cache_bind", "sva_cache_
             "sva_cache_release", "sva_select_context", "sva_pipeline_round", "sva_check_pipeline",
             "sva_rope_kv_write", "sva_rope_kv_write_qknorm", "sva_rope_kv_write_headnorm",
             "sva_attend_nodes",
-            "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_qkv_project",
+            "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_attend_weights", "sva_qkv_project",
             "sva_qkv_project_rope",
             "sva_attend_workspace_bytes",
             "sva_cache_set_workspace", "sva_attend_nodes_noalloc", "sva_poll_device_status",
@@ -110,6 +110,7 @@ def load(path: str = LIB_PATH):
         "sva_qkv_project": ([p, p, i32, i32, p, p, p, p, p, p], i32),
         "sva_qkv_project_rope": ([p, pn, i32, p, i32, p, p, p, p], i32),
         "sva_attend_nodes_masked": ([p, pn, i32, p, p, p, ctypes.c_float, p, p], i32),
+        "sva_attend_weights": ([p, pn, i32, p, p, ctypes.c_float, p, p, ctypes.c_float, p, p], i32),
         "sva_attend_workspace_bytes": ([p], ctypes.c_size_t),
         "sva_attend_nodes_noalloc": ([p, pn, i32, p, p, p, ctypes.c_float, p], i32),
         "sva_cache_set_workspace": ([p, p, ctypes.c_size_t], i32),
@@ -258,6 +259,7 @@ class Cache:
         self._scale = 1.0 / math.sqrt(self.d)
         self.T = g.frames * g.grid_h * g.grid_w
         self.Tpad = (self.T + 127) // 128 * 128
+        self._w_shape = (int(g.num_slots), self.H, self.T)
         handle = ctypes.c_void_p()
         with torch.cuda.device(buf.device):
             _check(lib.sva_cache_create(ctypes.byref(g), buf.data_ptr(),
@@ -387,6 +389,23 @@ class Cache:
                                           _stream_handle(stream))
         _check(st)
 
+    def _masks(self, count, tile_mask, own_mask, hist_mask) -> sva_attn_mask:
+        for t, nm, rows in ((tile_mask, "tile_mask", -(-self.T // 128)), (own_mask, "own_mask", self.T)):
+            if t is not None and (t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous()
+                                     or t.dim() != 3 or tuple(t.shape[:2]) != (count, rows)):
+                raise ValueError(f"{nm} must be a contiguous int32 CUDA tensor [{count}][{rows}][words]")
+        if hist_mask is not None and (hist_mask.dtype != torch.int32 or not hist_mask.is_cuda
+                                         or not hist_mask.is_contiguous() or hist_mask.dim() != 4
+                                         or tuple(hist_mask.shape[:2]) != (count, self.T)):
+            raise ValueError(f"hist_mask must be a contiguous int32 CUDA tensor [{count}][{self.T}][states][words]")
+        return sva_attn_mask(tile_mask.data_ptr() if tile_mask is not None else None,
+                             int(tile_mask.shape[2]) if tile_mask is not None else 0,
+                             own_mask.data_ptr() if own_mask is not None else None,
+                             int(own_mask.shape[2]) if own_mask is not None else 0,
+                             hist_mask.data_ptr() if hist_mask is not None else None,
+                             int(hist_mask.shape[2]) if hist_mask is not None else 0,
+                             int(hist_mask.shape[3]) if hist_mask is not None else 0)
+
     def attend_nodes_masked(self, nodes, q, out, lse=None, scale=None, tile_mask=None,
                             own_mask=None, hist_mask=None, stream=None, check=True):
         """sva_attend_nodes_masked: tile_mask as in attend_nodes_sparse, own_mask a
@@ -397,21 +416,7 @@ class Cache:
         if check:
             _tok_major(q, "q", count, self.T, self.H, self.d)
             _tok_major(out, "out", count, self.T, self.H, self.d)
-        for t, nm, rows in ((tile_mask, "tile_mask", -(-self.T // 128)), (own_mask, "own_mask", self.T)):
-            if t is not None and (t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous()
-                                  or t.dim() != 3 or tuple(t.shape[:2]) != (count, rows)):
-                raise ValueError(f"{nm} must be a contiguous int32 CUDA tensor [{count}][{rows}][words]")
-        if hist_mask is not None and (hist_mask.dtype != torch.int32 or not hist_mask.is_cuda
-                                      or not hist_mask.is_contiguous() or hist_mask.dim() != 4
-                                      or tuple(hist_mask.shape[:2]) != (count, self.T)):
-            raise ValueError(f"hist_mask must be a contiguous int32 CUDA tensor [{count}][{self.T}][states][words]")
-        m = sva_attn_mask(tile_mask.data_ptr() if tile_mask is not None else None,
-                          int(tile_mask.shape[2]) if tile_mask is not None else 0,
-                          own_mask.data_ptr() if own_mask is not None else None,
-                          int(own_mask.shape[2]) if own_mask is not None else 0,
-                          hist_mask.data_ptr() if hist_mask is not None else None,
-                          int(hist_mask.shape[2]) if hist_mask is not None else 0,
-                          int(hist_mask.shape[3]) if hist_mask is not None else 0)
+        m = self._masks(count, tile_mask, own_mask, hist_mask)
         if scale is None:
             scale = self._scale
         st = _lib.sva_attend_nodes_masked(self.handle, arr, count, q.data_ptr(),
@@ -420,6 +425,28 @@ class Cache:
                                           float(scale), ctypes.byref(m),
                                           _stream_handle(stream))
         _check(st)
+
+    def attend_weights(self, nodes, q, lse, out, prev=None, decay=1.0, scale=None, tile_mask=None,
+                       own_mask=None, hist_mask=None, stream=None, check=True):
+        """sva_attend_weights: the attention that every key of the slots the nodes see got from
+        their queries.  q, lse and the masks as in the attention call; out and prev fp32
+        [num_slots][H][T] (prev None: nothing before; it may be out itself)."""
+        arr, count = _node_array(nodes)
+        if check:
+            _tok_major(q, "q", count, self.T, self.H, self.d)
+            for t, nm, shape in ((lse, "lse", (count, self.H, self.T)), (out, "out", self._w_shape),
+                                 (prev, "prev", self._w_shape)):
+                if t is not None and (t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous()
+                                      or t.shape != shape):
+                    raise ValueError(f"{nm} must be a contiguous fp32 CUDA tensor {list(shape)}")
+        m = None
+        if tile_mask is not None or own_mask is not None or hist_mask is not None:
+            m = ctypes.byref(self._masks(count, tile_mask, own_mask, hist_mask))
+        _check(_lib.sva_attend_weights(
+            self.handle, arr, count, q.data_ptr(), lse.data_ptr(),
+            float(self._scale if scale is None else scale), m,
+            prev.data_ptr() if prev is not None else None, float(decay), out.data_ptr(),
+            _stream_handle(stream)))
 
     def qkv_project(self, x, weight, bias, q, k, v, stream=None, check=True):
         """sva_qkv_project: [q | k | v] = x W^T + b.  x [..., C] bf16 (rows = all
