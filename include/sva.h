@@ -384,6 +384,27 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
                               const float* lse, float scale, const sva_attn_mask* mask,
                               const float* prev, float decay, float* out, sva_stream s);
 
+/* Eviction by attention: makes one state of n_src, head by head.  Each head keeps,
+ * of the n_src * T tokens of the sources (candidate i * T + t: token t of source
+ * i), the T of largest weight; of equal ones the lowest candidates; NaN counts as
+ * the lowest weight.  Their K' and V rows, which carry the positions that they were
+ * written at, go to the destination slot in candidate order, their weights to its
+ * part of `weight`.  The destination is then a resident state like any other: the
+ * attention reads it in one slot where it read n_src.  The sources stay as they are
+ * (sva_cache_release frees them; their slots may be written again by later calls on
+ * the same stream).
+ *   src_slot  resident slots, distinct, 1..SVA_MAX_CTX of them
+ *   dst_slot  another slot, bound by the caller to a state of the same sequence
+ *             whose chunk is not before any source's (so that Eq. 4's causality
+ *             holds for what it contains)
+ *   weight    [num_slots][H][T] fp32, as sva_attend_weights accumulates it
+ *   index     [H][T] int32, receives the kept candidates in ascending order
+ * Stream-ordered.  Errors: INVALID_ARGUMENT, NOT_RESIDENT (a source), CAUSALITY (a
+ * source of another sequence or after the destination's chunk), CAPACITY (n_src),
+ * CUDA. */
+sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_src, int32_t dst_slot,
+                              float* weight, int32_t* index, sva_stream s);
+
 /* Bytes of the optional split workspace of a cache (0 if c is NULL).  With
  * a workspace attached, sva_attend_nodes may divide each (node, head,
  * query-tile pair) work unit into contiguous key ranges (up to 4, or up to 8

@@ -20,6 +20,7 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include "condense.h"
 #include "internal.h"
 #include "proj.h"
 #include "sva.h"
@@ -1381,6 +1382,55 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
   if (!p.masked && p.n_split == 1) grid = std::min<long long>(units, c->num_sms);
   cudaError_t e = sva::launch_weights(p, g.head_dim, (int)grid, reinterpret_cast<cudaStream_t>(s));
   if (e != cudaSuccess) return cuda_fail(e, "attend_weights launch");
+  return ok();
+}
+
+sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_src, int32_t dst_slot,
+                              float* weight, int32_t* index, sva_stream s) {
+  if (c == nullptr || src_slot == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  if (n_src < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_src %d < 1", n_src);
+  if (n_src > SVA_MAX_CTX)
+    return fail(SVA_ERR_CAPACITY, "n_src %d > SVA_MAX_CTX (%d)", n_src, SVA_MAX_CTX);
+  if (weight == nullptr || index == nullptr || (reinterpret_cast<uintptr_t>(weight) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(index) & 3u) != 0)
+    return fail(SVA_ERR_INVALID_ARGUMENT, "weight and index must be non-NULL and 4-byte aligned");
+  sva_status st = check_device(c);
+  if (st != SVA_OK) return st;
+  const sva_geometry& g = c->g;
+  if (dst_slot < 0 || dst_slot >= g.num_slots || !c->slots[dst_slot].bound)
+    return fail(SVA_ERR_INVALID_ARGUMENT, "dst_slot %d is not a bound slot", dst_slot);
+  const SlotInfo& dst = c->slots[dst_slot];
+  sva::CondenseParams p{};
+  for (int i = 0; i < n_src; ++i) {
+    const int32_t slot = src_slot[i];
+    if (slot < 0 || slot >= g.num_slots)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "source %d: slot %d out of range", i, slot);
+    const SlotInfo& si = c->slots[slot];
+    if (!si.bound || !si.resident)
+      return fail(SVA_ERR_NOT_RESIDENT, "source %d: slot %d is %s", i, slot,
+                  si.bound ? "bound but not written" : "not bound");
+    if (slot == dst_slot) return fail(SVA_ERR_INVALID_ARGUMENT, "source %d is the destination", i);
+    for (int k = 0; k < i; ++k)
+      if (src_slot[k] == slot) return fail(SVA_ERR_INVALID_ARGUMENT, "slot %d listed twice", slot);
+    if (si.seq != dst.seq || si.chunk > dst.chunk)
+      return fail(SVA_ERR_CAUSALITY,
+                  "source %d holds (seq %d, chunk %d): not of the destination's sequence %d, or after "
+                  "its chunk %d",
+                  i, si.seq, si.chunk, dst.seq, dst.chunk);
+    p.slot[i] = slot;
+  }
+  p.weight = weight;
+  p.index = index;
+  p.pool = c->base;
+  p.T = c->L.T;
+  p.Tpad = c->L.Tpad;
+  p.H = g.num_heads;
+  p.d = g.head_dim;
+  p.n_src = n_src;
+  p.dst = dst_slot;
+  cudaError_t e = sva::launch_condense(p, reinterpret_cast<cudaStream_t>(s));
+  if (e != cudaSuccess) return cuda_fail(e, "condense launch");
+  c->slots[dst_slot].resident = true;
   return ok();
 }
 

@@ -39,7 +39,8 @@ EXPORTED = ("sva_cache_bytes", "sva_cache_create", "sva_cache_bind", "sva_cache_
             "sva_cache_release", "sva_select_context", "sva_pipeline_round", "sva_check_pipeline",
             "sva_rope_kv_write", "sva_rope_kv_write_qknorm", "sva_rope_kv_write_headnorm",
             "sva_attend_nodes",
-            "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_attend_weights", "sva_qkv_project",
+            "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_attend_weights", "sva_cache_condense",
+            "sva_qkv_project",
             "sva_qkv_project_rope",
             "sva_attend_workspace_bytes",
             "sva_cache_set_workspace", "sva_attend_nodes_noalloc", "sva_poll_device_status",
@@ -111,6 +112,7 @@ def load(path: str = LIB_PATH):
         "sva_qkv_project_rope": ([p, pn, i32, p, i32, p, p, p, p], i32),
         "sva_attend_nodes_masked": ([p, pn, i32, p, p, p, ctypes.c_float, p, p], i32),
         "sva_attend_weights": ([p, pn, i32, p, p, ctypes.c_float, p, p, ctypes.c_float, p, p], i32),
+        "sva_cache_condense": ([p, pi32, i32, i32, p, p, p], i32),
         "sva_attend_workspace_bytes": ([p], ctypes.c_size_t),
         "sva_attend_nodes_noalloc": ([p, pn, i32, p, p, p, ctypes.c_float, p], i32),
         "sva_cache_set_workspace": ([p, p, ctypes.c_size_t], i32),
@@ -447,6 +449,19 @@ class Cache:
             float(self._scale if scale is None else scale), m,
             prev.data_ptr() if prev is not None else None, float(decay), out.data_ptr(),
             _stream_handle(stream)))
+
+    def condense(self, src_slots, dst_slot, weight, index, stream=None, check=True):
+        """sva_cache_condense: keeps, head by head, the T tokens of largest weight of the source slots
+        in the destination slot.  weight fp32 [num_slots][H][T], index int32 [H][T] (the kept
+        candidates: source i, token t as i * T + t)."""
+        if check:
+            for t, nm, dt, shape in ((weight, "weight", torch.float32, self._w_shape),
+                                     (index, "index", torch.int32, self._w_shape[1:])):
+                if t.dtype != dt or not t.is_cuda or not t.is_contiguous() or t.shape != shape:
+                    raise ValueError(f"{nm} must be a contiguous {dt} CUDA tensor {list(shape)}")
+        n = len(src_slots)
+        _check(_lib.sva_cache_condense(self.handle, (ctypes.c_int32 * max(n, 1))(*src_slots), n, dst_slot,
+                                       weight.data_ptr(), index.data_ptr(), _stream_handle(stream)))
 
     def qkv_project(self, x, weight, bias, q, k, v, stream=None, check=True):
         """sva_qkv_project: [q | k | v] = x W^T + b.  x [..., C] bf16 (rows = all
