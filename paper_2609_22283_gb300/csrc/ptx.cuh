@@ -95,10 +95,13 @@ __device__ __forceinline__ void ffma2(float& o0, float& o1, float a0, float a1, 
   u2f(r, o0, o1);
 }
 
-__device__ __forceinline__ uint64_t fadd2(uint64_t a, float b0, float b1) {
+__device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
   uint64_t r;
-  asm("add.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(f2u(b0, b1)));
+  asm("add.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+__device__ __forceinline__ uint64_t fadd2(uint64_t a, float b0, float b1) {
+  return fadd2(a, f2u(b0, b1));
 }
 
 // ---------------------------------------------------------------- mbarrier

@@ -391,6 +391,35 @@ constexpr long long kScanItems = 4;
 // tile.
 constexpr long long kScanMinTiles = 12000;
 
+// Bytes of the scan of a launch's token masks in the tail of the workspace, 0 where
+// there is none to take them or it has no room.  max_states: 1 + the largest n_ctx.
+size_t scan_room(const sva_cache* c, const sva_attn_mask& m, int n_nodes, int max_states) {
+  if ((m.own_mask == nullptr && m.hist_mask == nullptr) || c->ws == nullptr) return 0;
+  const size_t nt = c->L.Tpad / sva::kTile;
+  const size_t bytes = round_up((size_t)n_nodes * nt * max_states * nt, 256);
+  return bytes <= (size_t)kScanItems * ws_item_bytes(c) ? bytes : 0;
+}
+
+// Launches that scan: *any[(node, query tile)][key tile in the order of a tile
+// mask], rows of *stride bytes.
+cudaError_t launch_scan(const sva_cache* c, const sva_attn_mask& m, const sva_node* nodes, int n_nodes,
+                        int max_states, size_t bytes, cudaStream_t s, const uint8_t** any, int32_t* stride) {
+  static thread_local sva::ScanParams sp;
+  sp.own_mask = m.own_mask;
+  sp.hist_mask = m.hist_mask;
+  sp.own_words = m.own_words;
+  sp.hist_states = m.hist_states;
+  sp.hist_words = m.hist_words;
+  sp.T = c->L.T;
+  sp.n_qt = c->L.Tpad / sva::kTile;
+  sp.any = reinterpret_cast<uint8_t*>(c->ws) + ws_total_bytes(c) - bytes;
+  sp.row_bytes = max_states * sp.n_qt;
+  for (int i = 0; i < n_nodes; ++i) sp.n_ctx[i] = nodes[i].n_ctx;
+  *any = sp.any;
+  *stride = sp.row_bytes;
+  return sva::launch_mask_scan(sp, n_nodes, max_states, s);
+}
+
 // Fewest key tiles a work unit of node i walks: all of its slots' tiles,
 // except under frame causality, where a pair of query tiles skips the own
 // chunk's tiles past its last row's frame (the first pair skips the most).
@@ -944,14 +973,9 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
   int max_states = 1;
   for (int i = 0; i < n_nodes; ++i) max_states = std::max(max_states, 1 + nodes[i].n_ctx);
   size_t scan_bytes = 0;
-  if ((p.own_mask != nullptr || p.hist_mask != nullptr) && c->ws != nullptr &&
-      scratch == Scratch::kWorkspace && units * min_tiles >= kScanMinTiles) {
-    const size_t bytes = round_up((size_t)n_nodes * p.n_qt * max_states * p.nt_slot, 256);
-    const long long items = (long long)((bytes + ws_item_bytes(c) - 1) / ws_item_bytes(c));
-    if (items <= kScanItems) {
-      scan_bytes = bytes;
-      cap -= items;
-    }
+  if (scratch == Scratch::kWorkspace && units * min_tiles >= kScanMinTiles) {
+    scan_bytes = scan_room(c, mask, n_nodes, max_states);
+    cap -= (long long)((scan_bytes + ws_item_bytes(c) - 1) / ws_item_bytes(c));
   }
   LaunchPlan plan;
   // Pair-major order costs the L2 reuse of a head's K/V by the CTAs that run
@@ -1050,20 +1074,8 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
   // Token masks: reduce them to the key tiles they leave anything of, in the
   // last scan_bytes of the workspace (the split items end before, see `cap`).
   if (scan_bytes > 0) {
-    static thread_local sva::ScanParams sp;
-    sp.own_mask = p.own_mask;
-    sp.hist_mask = p.hist_mask;
-    sp.own_words = p.own_words;
-    sp.hist_states = p.hist_states;
-    sp.hist_words = p.hist_words;
-    sp.T = c->L.T;
-    sp.n_qt = p.n_qt;
-    sp.any = reinterpret_cast<uint8_t*>(c->ws) + ws_total_bytes(c) - scan_bytes;
-    sp.row_bytes = max_states * p.nt_slot;
-    for (int i = 0; i < n_nodes; ++i) sp.n_ctx[i] = nodes[i].n_ctx;
-    p.any_tile = sp.any;
-    p.any_stride = sp.row_bytes;
-    cudaError_t e = sva::launch_mask_scan(sp, n_nodes, max_states, reinterpret_cast<cudaStream_t>(s));
+    cudaError_t e = launch_scan(c, mask, nodes, n_nodes, max_states, scan_bytes,
+                                reinterpret_cast<cudaStream_t>(s), &p.any_tile, &p.any_stride);
     if (e != cudaSuccess) return cuda_fail(e, "mask scan launch");
   }
   const long long grid = n_full + (units - n_full) * n_split;
@@ -1380,6 +1392,19 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
   p.n_split = (int32_t)std::max(1ll, std::min({(long long)sva::kMaxWeightSplit, c->num_sms / units, tiles / 2}));
   long long grid = units * p.n_split;
   if (!p.masked && p.n_split == 1) grid = std::min<long long>(units, c->num_sms);
+  // Token masks are scanned for the tiles they leave anything of where the walk of
+  // all tiles is about as long as that of the attention's rule: a Q tile past a pair
+  // of key tiles takes about 0.9 us.
+  int max_states = 1;
+  for (int i = 0; i < n_nodes; ++i) max_states = std::max(max_states, 1 + nodes[i].n_ctx);
+  if ((long long)refs * p.n_qt * g.num_heads * p.n_pairs >= kScanMinTiles) {
+    const size_t bytes = scan_room(c, m, n_nodes, max_states);
+    if (bytes > 0) {
+      cudaError_t e = launch_scan(c, m, nodes, n_nodes, max_states, bytes, reinterpret_cast<cudaStream_t>(s),
+                                  &p.any_tile, &p.any_stride);
+      if (e != cudaSuccess) return cuda_fail(e, "mask scan launch");
+    }
+  }
   cudaError_t e = sva::launch_weights(p, g.head_dim, (int)grid, reinterpret_cast<cudaStream_t>(s));
   if (e != cudaSuccess) return cuda_fail(e, "attend_weights launch");
   return ok();

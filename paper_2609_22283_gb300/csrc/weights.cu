@@ -49,28 +49,50 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 384;
-constexpr int kStages = 4;  // Q tiles in flight
-constexpr int kGroupWarps = 4;
+constexpr int kThreads = 640;
+constexpr int kRing = 3;  // S buffers and stages of log-sum-exps: item i uses number i % 3
+constexpr int kMaxStages = 8;
+constexpr int kGroupWarps = 8;
 
 template <int D>
 struct Cfg {
   static constexpr int kBoxBytes = kTile * 64 * 2;  // one 128-row x 64-column bf16 box
   static constexpr int kBoxes = D / 64;
   static constexpr int kTileBytes = kBoxBytes * kBoxes;
+  static constexpr int kStages = D == 128 ? 4 : 8;  // Q tiles in flight
   static constexpr int kOffK = kStages * kTileBytes;
   static constexpr int kSmemBytes = kOffK + 2 * kTileBytes + 1024;  // + alignment slack
   static constexpr uint32_t kKCols = D / 2;          // TMEM columns of a K tile
   static constexpr uint32_t kColS = 128;             // first S buffer
 };
 
+// Position in the rings of three: i % 3 and the parity of i / 3.
+struct Ring {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step() {
+    ++at;
+    if (at == 3) {
+      at = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// What goes with a Q tile, and the barriers of number i % 3 of the rings.
+struct alignas(16) Stage {
+  float nl[kTile];      // -lse * log2(e) of its queries
+  uint64_t l_full;      // nl is there
+  uint64_t l_empty;     // both groups are done with it
+  uint64_t s_full[2], s_empty[2];  // S of each group
+};
+
 struct Bars {
-  uint64_t q_full[kStages];   // the Q tile has landed
-  uint64_t l_full[kStages];   // its log-sum-exps (and mask words) are there
-  uint64_t q_empty[kStages];  // both groups are done with the stage
+  uint64_t q_full[kMaxStages];   // a Q tile has landed
+  uint64_t q_empty[kMaxStages];  // both groups' MMAs have read it
   uint64_t k_full, k_empty;   // K tiles of a unit in shared memory
   uint64_t k_ready[2];        // K tile in TMEM
-  uint64_t s_full[2][3], s_empty[2][3];
+  uint64_t t_full[2], t_empty[2];  // the second half's sums of a unit
   uint64_t drain;
 };
 
@@ -94,6 +116,17 @@ __device__ __forceinline__ void mma_ts_kmajor_x4(uint32_t d_tmem, uint32_t a_tme
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar, int32_t c0,
                                             int32_t c1) {
   asm volatile(
@@ -117,10 +150,26 @@ struct Walk {
   int at, end, n_qt, r, qt;
   uint32_t left;
   __device__ __forceinline__ Walk(const uint32_t* marks_, int begin, int end_, int n_qt_)
-      : marks(marks_), at(begin), end(end_), n_qt(n_qt_), r(begin / n_qt_), qt(begin - r * n_qt_), left(0) {
+      : marks(marks_), at(begin), end(end_), n_qt(n_qt_), r(begin > 0 ? begin / n_qt_ : 0), qt(begin - r * n_qt_), left(0) {
     if constexpr (kMask) {
       left = begin < end ? marks[begin >> 5] & (~0u << (begin & 31)) : 0u;
       at = begin >> 5;
+    }
+  }
+  // How many there are (before the first next).
+  __device__ __forceinline__ int count() const {
+    if constexpr (kMask) {
+      if (at * 32 >= end) return 0;
+      int n = 0;
+      const int words = (end + 31) >> 5;
+      for (int w = at; w < words; ++w) {
+        uint32_t m = w == at ? left : marks[w];
+        if (w == words - 1 && (end & 31)) m &= (1u << (end & 31)) - 1u;
+        n += __popc(m);
+      }
+      return n;
+    } else {
+      return end - at;
     }
   }
   // The next item into (r, qt); false past the last.
@@ -155,12 +204,12 @@ struct Unit {
   int si, h, kp;  // index of the slot in the launch's list, head, pair of key tiles
 };
 __device__ __forceinline__ Unit unit_of(const WeightParams& p, int u) {
-  const int per_slot = p.H * p.n_pairs;
+  const uint32_t per_slot = (uint32_t)(p.H * p.n_pairs);
   Unit x;
-  x.si = u / per_slot;
-  const int r = u - x.si * per_slot;
-  x.h = r / p.n_pairs;
-  x.kp = r - x.h * p.n_pairs;
+  x.si = (int)((uint32_t)u / per_slot);
+  const uint32_t r = (uint32_t)u - (uint32_t)x.si * per_slot;
+  x.h = (int)(r / (uint32_t)p.n_pairs);
+  x.kp = (int)r - x.h * p.n_pairs;
   return x;
 }
 
@@ -178,13 +227,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   __shared__ Bars bars;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
-  __shared__ alignas(16) float nl[kStages][kTile];  // -lse * log2(e) of a stage's queries
-  // masks: word w of key tile kt for each query of the stage; 0 none, 1 some, 2 all
-  // of a tile's pairs visible; the Q tiles that the unit walks
-  __shared__ alignas(16) uint32_t vis[kMask ? kStages : 1][2][4][kMask ? kTile : 1];
-  __shared__ int seen[kMask ? kStages : 1][2];
+  __shared__ Stage stage[kRing];
   __shared__ uint32_t marks[kMask ? SVA_MAX_NODES * kMaxQueryTiles / 32 : 1];
   __shared__ float part[kMaxWeightSplit][2 * kTile];  // rank 0: the cluster's partial sums
+  __shared__ float half_sum[2][kTile];                // the second half's sums of a unit
   __shared__ volatile float part_lost;                // rank 0: a CTA of the cluster gave up
 
   const int warp = threadIdx.x >> 5;
@@ -202,19 +248,24 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     prefetch_tmap(&p.tmap_kv);
     abort_flag = 0;
     part_lost = 0.0f;
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&bars.q_full[s], 1);
-      mbar_init(&bars.l_full[s], 1);
-      mbar_init(&bars.q_empty[s], 2 * kGroupWarps);
+      mbar_init(&bars.q_empty[s], 2);
+    }
+    for (int s = 0; s < kRing; ++s) {
+      mbar_init(&stage[s].l_full, 1);
+      mbar_init(&stage[s].l_empty, 2 * kGroupWarps * 32);
+      for (int k = 0; k < 2; ++k) {
+        mbar_init(&stage[s].s_full[k], 1);
+        mbar_init(&stage[s].s_empty[k], kGroupWarps * 32);
+      }
     }
     mbar_init(&bars.k_full, 1);
     mbar_init(&bars.k_empty, 2 * kGroupWarps);
     for (int k = 0; k < 2; ++k) {
       mbar_init(&bars.k_ready[k], kGroupWarps);
-      for (int j = 0; j < 3; ++j) {
-        mbar_init(&bars.s_full[k][j], 1);
-        mbar_init(&bars.s_empty[k][j], kGroupWarps);
-      }
+      mbar_init(&bars.t_full[k], kGroupWarps / 2 * 32);
+      mbar_init(&bars.t_empty[k], kGroupWarps / 2 * 32);
     }
     mbar_init(&bars.drain, 2);
     fence_mbar_init();
@@ -245,6 +296,11 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           on = ((row[k >> 5] >> (k & 31)) & 1u) != 0u;
           if (2 * un.kp + 1 < p.n_qt) on = on || ((row[(k + 1) >> 5] >> ((k + 1) & 31)) & 1u) != 0u;
         }
+        if (p.any_tile) {
+          const uint8_t* row = p.any_tile + ((size_t)(ref & 63) * p.n_qt + qt) * p.any_stride;
+          const int k = state * p.n_qt + 2 * un.kp;
+          on = on && (row[k] != 0 || (2 * un.kp + 1 < p.n_qt && row[k + 1] != 0));
+        }
         if (state == 0 && (ref & kRefCausal)) {
           const int last = min((qt + 1) * kTile, p.T) - 1;
           on = on && last / p.frame_tokens >= 2 * un.kp * kTile / p.frame_tokens;
@@ -262,9 +318,13 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
 
   // The Q tiles [begin, end) of a unit that this CTA takes.
   auto walk_of = [&](const Unit& un) {
-    const int n_all = (p.first[un.si + 1] - p.first[un.si]) * p.n_qt;
-    return Walk<kMask>(marks, (int)((long long)n_all * rank / ns), (int)((long long)n_all * (rank + 1) / ns),
-                       p.n_qt);
+    const uint32_t n_all = (uint32_t)(p.first[un.si + 1] - p.first[un.si]) * (uint32_t)p.n_qt;  // < 2^16
+    uint32_t begin = 0, end = n_all;
+    if (ns > 1) {
+      begin = n_all * (uint32_t)rank / (uint32_t)ns;
+      end = n_all * (uint32_t)(rank + 1) / (uint32_t)ns;
+    }
+    return Walk<kMask>(marks, (int)begin, (int)end, p.n_qt);
   };
 
   int q_issued = 0, k_issued = 0;  // producer: copies started
@@ -291,8 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         int r, qt;
         while (walk.next(r, qt)) {
           const int node = p.ref[p.first[un.si] + r] & 63;
-          const int st = q_issued % kStages;
-          ok = mbar_wait(&bars.q_empty[st], ((uint32_t)(q_issued / kStages) & 1u) ^ 1u, &abort_flag, tmo);
+          const int st = q_issued % C::kStages;
+          ok = mbar_wait(&bars.q_empty[st], ((uint32_t)(q_issued / C::kStages) & 1u) ^ 1u, &abort_flag, tmo);
           if (!ok) break;
           // fault_mode 2 (test hook): withhold the copy of the second tile
           if (!(p.fault_mode == 2 && q_issued == 1)) {
@@ -308,92 +368,44 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       if (!ok) record_timeout(p, &abort_flag);
     }
   } else if (warp == 2) {
-    // ------------------------------------------------------------ log-sum-exps and mask words
-    bool ok = true;
-    int it = 0;
-    for (int u = u0; ok && u < p.units; u += u_step) {
-      const Unit un = unit_of(p, u);
-      Walk<kMask> walk = walk_of(un);
+    // ------------------------------------------------------------ log-sum-exps
+    // Loaded an item ahead of their stage.
+    int u = u0;
+    Unit un = unit_of(p, u < p.units ? u : 0);
+    Walk<kMask> walk = walk_of(un);
+    float v[4];  // of queries k * 32 + lane
+    auto load = [&]() {  // the next item's; false past the last
+      if (u >= p.units) return false;
       int r, qt;
-      while (walk.next(r, qt)) {
-        const uint32_t ref = p.ref[p.first[un.si] + r];
-        const int node = (int)(ref & 63u);
-        const float* src = p.lse + ((size_t)node * p.H + un.h) * p.T;
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int row = qt * kTile + k * 32 + lane;
-          v[k] = ld_f32_if(src + row, row < p.T, INFINITY);
-        }
-        const int st = it % kStages;
-        uint32_t w[kMask ? 4 : 1][8];  // of query k * 32 + lane: four words of each key tile
-        if constexpr (kMask) {
-          const int state = (int)(ref >> kRefStateShift) & 31;
-          const uint32_t* base = state == 0 ? p.own_mask : p.hist_mask;
-          const int words = (p.T + 31) / 32;
-          const int w0 = un.kp * 8;  // first word of the pair of key tiles
-          bool tile_on[2] = {true, true};
-          if (p.tile_mask) {
-            const uint32_t* row = p.tile_mask + ((size_t)node * p.n_qt + qt) * p.mask_words;
-            const int k = state * p.n_qt + 2 * un.kp;
-            tile_on[0] = ((row[k >> 5] >> (k & 31)) & 1u) != 0u;
-            if (2 * un.kp + 1 < p.n_qt) tile_on[1] = ((row[(k + 1) >> 5] >> ((k + 1) & 31)) & 1u) != 0u;
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int q = qt * kTile + k * 32 + lane;
-            const size_t qrow = (size_t)node * p.T + q;
-            const uint32_t* row = state == 0 ? base + qrow * p.own_words
-                                             : base + (qrow * p.hist_states + (state - 1)) * p.hist_words;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              w[k][j] = ld_global_u32_if(row + w0 + j, base != nullptr && q < p.T && w0 + j < words, ~0u);
-            int upto = p.T;  // keys that the frames leave visible
-            if (state == 0 && (ref & kRefCausal)) upto = (q / p.frame_tokens + 1) * p.frame_tokens;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int n = upto - (w0 + j) * 32;
-              if (n < 32) w[k][j] &= n <= 0 ? 0u : (1u << n) - 1u;
-              // keys past T have no sum: they count as visible so that a whole
-              // tile of a ragged slot can be one
-              const int past = p.T - (w0 + j) * 32;
-              if (past < 32) w[k][j] |= past <= 0 ? ~0u : ~0u << past;
-              // a query that saw nothing adds nothing, whatever its row holds,
-              // nor do the rows past T to a key that no query sees
-              if (!tile_on[j >> 2] || v[k] == -INFINITY || q >= p.T) w[k][j] = 0u;
-            }
-          }
-        }
-        if (!__all_sync(0xffffffffu, mbar_wait(&bars.q_empty[st], ((uint32_t)(it / kStages) & 1u) ^ 1u,
-                                               &abort_flag, tmo))) {
-          ok = false;
-          break;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          nl[st][k * 32 + lane] = v[k] == -INFINITY ? -INFINITY : v[k] * -1.4426950408889634f;
-        if constexpr (kMask) {
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt) {
-            uint32_t any = 0u, all = ~0u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t x = w[k][kt * 4 + j];
-                vis[st][kt][j][k * 32 + lane] = x;
-                any |= x;
-                all &= x;
-              }
-            any = __reduce_or_sync(0xffffffffu, any);
-            all = __reduce_and_sync(0xffffffffu, all);
-            if (lane == 0) seen[st][kt] = any == 0u ? 0 : (all == ~0u ? 2 : 1);
-          }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.l_full[st]);
-        ++it;
+      while (!walk.next(r, qt)) {
+        u += u_step;
+        if (u >= p.units) return false;
+        un = unit_of(p, u);
+        walk = walk_of(un);
       }
+      const int node = p.ref[p.first[un.si] + r] & 63;
+      const float* src = p.lse + ((size_t)node * p.H + un.h) * p.T;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int row = qt * kTile + k * 32 + lane;
+        v[k] = ld_f32_if(src + row, row < p.T, INFINITY);
+      }
+      return true;
+    };
+    bool ok = true;
+    bool more = load();
+    Ring it;
+    while (more) {
+      Stage& g = stage[it.at];
+      ok = __all_sync(0xffffffffu, mbar_wait(&g.l_empty, it.phase ^ 1u, &abort_flag, tmo)) != 0;
+      if (!ok) break;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        g.nl[k * 32 + lane] = v[k] == -INFINITY ? -INFINITY : v[k] * -1.4426950408889634f;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&g.l_full);
+      it.step();
+      more = load();
     }
     if (!ok && lane == 0) record_timeout(p, &abort_flag);
   } else if (warp < 4) {
@@ -406,48 +418,61 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       return __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_flag, tmo)) != 0;
     };
     bool ok = true;
-    int it = 0, n_unit = 0;
-    int buf = kt;  // S buffer of step 2 * it + kt
+    int n_unit = 0, qs = 0;
+    uint32_t q_phase = 0;
+    Ring it, other;             // this item; the other group's item that had the S buffer before
+    bool reused = false;        // there was one
+    int ahead = kt == 1 ? 1 : 2;  // items until then
+    int buf = kt;               // S buffer of step 2 * it + kt
     for (int u = u0; ok && u < p.units; u += u_step, ++n_unit) {
       const Unit un = unit_of(p, u);
+      Walk<kMask> walk = walk_of(un);
       ok = wait(&bars.k_ready[kt], (uint32_t)n_unit & 1u);
       if (!ok) break;
-      Walk<kMask> walk = walk_of(un);
       int r, qt;
       while (walk.next(r, qt)) {
-        const int st = it % kStages;
-        // the buffer's last user: the other group, 1 (kt = 1) or 2 items ago
-        const int before = it - (kt == 1 ? 1 : 2);
-        ok = wait(&bars.q_full[st], (uint32_t)(it / kStages) & 1u) &&
-             (before < 0 || wait(&bars.s_empty[1 - kt][before % 3], (uint32_t)(before / 3) & 1u));
+        if (!reused) reused = ahead-- == 0;
+        ok = wait(&bars.q_full[qs], q_phase);
+        if (ok && reused) {
+          ok = wait(&stage[other.at].s_empty[1 - kt], other.phase);
+          other.step();
+        }
         if (!ok) break;
         tc_fence_after();
         const uint32_t dcol = tbase + C::kColS + (uint32_t)buf * kTile;
-        const uint64_t b = dQ + (uint64_t)(st * (C::kTileBytes >> 4));
+        const uint64_t b = dQ + (uint64_t)(qs * (C::kTileBytes >> 4));
 #pragma unroll
         for (int x = 0; x < C::kBoxes; ++x)
           mma_ts_kmajor_x4(dcol, kcol + x * 32, b + (uint64_t)(x * (C::kBoxBytes >> 4)), idesc, x > 0 ? 1u : 0u);
-        mma_commit_warp(&bars.s_full[kt][it % 3]);
+        mma_commit_warp(&stage[it.at].s_full[kt]);
+        mma_commit_warp(&bars.q_empty[qs]);
+        if (++qs == C::kStages) {
+          qs = 0;
+          q_phase ^= 1u;
+        }
         buf = buf == 0 ? 2 : buf - 1;  // two steps on, modulo 3
-        ++it;
+        it.step();
       }
     }
     if (!ok && lane == 0) record_timeout(p, &abort_flag);
   } else {
     // ------------------------------------------------------------ sums
-    const int kt = (warp - 4) >> 2;
+    const int kt = (warp - 4) >> 3;
+    const int half = ((warp - 4) >> 2) & 1;  // which 64 queries of a Q tile
     const int q4 = warp & 3;  // TMEM lane quarter this warp may access
     const int row = q4 * 32 + lane;
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
     const uint64_t sl2x2 = f2u(p.scale_log2, p.scale_log2);
     bool ok = true;
-    int n_unit = 0, it = 0, buf = kt;
+    int n_unit = 0, done = 0, buf = kt;
+    Ring it;
     // This thread's row of the next unit's K, shared memory -> TMEM.
     auto copy_k = [&]() {
       if (!__all_sync(0xffffffffu, mbar_wait(&bars.k_full, (uint32_t)n_unit & 1u, &abort_flag, tmo))) return false;
       const uint32_t at = smem_u32(smem + C::kOffK + kt * C::kTileBytes) + (uint32_t)(row * 128);
 #pragma unroll
       for (int b = 0; b < C::kBoxes; ++b) {
+        if (b != half) continue;
         uint32_t w[32];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -475,89 +500,166 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       const bool has_keys = key - lane < p.T;  // this warp's part of the tile; K is not loaded past the slot
       const float before = ld_f32_if(p.prev + at, p.prev != nullptr && mine && ns == 1, 0.0f);
       float total = 0.0f;
+      const bool next_k = u + u_step < p.units;  // another unit's K is to follow
       Walk<kMask> walk = walk_of(un);
-      int r, qt;
-      bool more = walk.next(r, qt);
-      bool next_k = u + u_step < p.units;  // another unit's K is to follow
-      if (!more && next_k) {               // no Q tile (masks only): nothing reads this K
+      int left = walk.count();
+      if (left == 0 && next_k) {  // no Q tile (masks only): nothing reads this K
         ok = copy_k();
         if (!ok) break;
       }
-      while (more) {
-        const int st = it % kStages;
-        if (!__all_sync(0xffffffffu,
-                        mbar_wait(&bars.l_full[st], (uint32_t)(it / kStages) & 1u, &abort_flag, tmo) &&
-                            mbar_wait(&bars.s_full[kt][it % 3], (uint32_t)(it / 3) & 1u, &abort_flag, tmo))) {
-          ok = false;
-          break;
+      // Masks: this warp's 32 keys for query half * 64 + c * 32 + lane of the item,
+      // a bit a key, loaded an item ahead.
+      uint32_t seen[2] = {0u, 0u}, seen_next[2] = {0u, 0u};
+      auto load_seen = [&]() {
+        int r, qt;
+        if (!walk.next(r, qt)) return;
+        const uint32_t ref = p.ref[p.first[un.si] + r];
+        const int node = (int)(ref & 63u), state = (int)(ref >> kRefStateShift) & 31;
+        const int key0 = key - lane;
+        bool tile_on = true;
+        if (p.tile_mask) {
+          const uint32_t* row_m = p.tile_mask + ((size_t)node * p.n_qt + qt) * p.mask_words;
+          const int k = state * p.n_qt + 2 * un.kp + kt;
+          tile_on = has_keys && ((row_m[k >> 5] >> (k & 31)) & 1u) != 0u;
+        }
+        const uint32_t* base = state == 0 ? p.own_mask : p.hist_mask;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int q = qt * kTile + half * 64 + c * 32 + lane;
+          const size_t qrow = (size_t)node * p.T + q;
+          const uint32_t* w = state == 0 ? base + qrow * p.own_words
+                                         : base + (qrow * p.hist_states + (state - 1)) * p.hist_words;
+          const bool on = tile_on && has_keys && q < p.T;
+          seen_next[c] = ld_global_u32_if(w + (key0 >> 5), base != nullptr && on, on ? ~0u : 0u);
+          if (state == 0 && (ref & kRefCausal)) {  // keys up to the end of the query's frame
+            const int n = (q / p.frame_tokens + 1) * p.frame_tokens - key0;
+            if (n < 32) seen_next[c] &= n <= 0 ? 0u : (1u << n) - 1u;
+          }
+        }
+      };
+      if constexpr (kMask) load_seen();
+      while (left > 0) {
+        Stage& g = stage[it.at];
+        if constexpr (kMask) {
+          seen[0] = seen_next[0];
+          seen[1] = seen_next[1];
+          load_seen();
+        }
+        // both normally tested in one round trip
+        const bool lok = mbar_try_wait(&g.l_full, it.phase);
+        const bool sok = mbar_try_wait(&g.s_full[kt], it.phase);
+        if (!__all_sync(0xffffffffu, lok && sok)) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&g.l_full, it.phase, &abort_flag, tmo) &&
+                                           mbar_wait(&g.s_full[kt], it.phase, &abort_flag, tmo));
+          if (!ok) break;
         }
         tc_fence_after();
-        more = walk.next(r, qt);
-        if (!more && next_k) {  // the unit's last S is complete: no MMA reads its K any more
+        --left;
+        if (left == 0 && next_k) {  // the unit's last S is complete: no MMA reads its K any more
           ok = copy_k();
           if (!ok) break;
         }
-        const int look = !has_keys ? 0 : kMask ? seen[st][kt] : 2;
-        const uint32_t scol = tbase + lane_off + C::kColS + (uint32_t)buf * kTile;
         uint64_t acc[4] = {0, 0, 0, 0};
-        auto add = [&](const uint32_t (&s)[32], int c) {
-          const ulonglong2* nl2 = reinterpret_cast<const ulonglong2*>(&nl[st][c * 32]);
-          const uint4* vw = reinterpret_cast<const uint4*>(&vis[kMask ? st : 0][kt][q4][kMask ? c * 32 : 0]);
+        // The 16 queries from half * 64 + c * 16 on; with masks those whose bit is set.
+        auto add = [&](const uint32_t (&s)[16], int c, bool some, uint32_t bits) {
+          const ulonglong2* nl2 = reinterpret_cast<const ulonglong2*>(&g.nl[half * 64 + c * 16]);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
+          for (int e = 0; e < 16; e += 4) {
             const ulonglong2 n = nl2[e >> 2];
             float x0, x1, x2, x3;
             ffma2(x0, x1, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), sl2x2, n.x);
             ffma2(x2, x3, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]), sl2x2, n.y);
-            if constexpr (kMask) {
-              if (look == 1) {
-                const uint4 v = vw[e >> 2];
-                if (!((v.x >> lane) & 1u)) x0 = -INFINITY;
-                if (!((v.y >> lane) & 1u)) x1 = -INFINITY;
-                if (!((v.z >> lane) & 1u)) x2 = -INFINITY;
-                if (!((v.w >> lane) & 1u)) x3 = -INFINITY;
-              }
+            if (some) {
+              if (!((bits >> e) & 1u)) x0 = -INFINITY;
+              if (!((bits >> (e + 1)) & 1u)) x1 = -INFINITY;
+              if (!((bits >> (e + 2)) & 1u)) x2 = -INFINITY;
+              if (!((bits >> (e + 3)) & 1u)) x3 = -INFINITY;
             }
             acc[(e >> 1) & 3] = fadd2(acc[(e >> 1) & 3], ex2(x0), ex2(x1));
             acc[((e >> 1) + 1) & 3] = fadd2(acc[((e >> 1) + 1) & 3], ex2(x2), ex2(x3));
           }
         };
-        uint32_t s0[32], s1[32];
-        if (look != 0) {
-          tmem_ld32(scol, s0);
-          tmem_ld32(scol + 32, s1);
-          tmem_wait_ld(s0);
-          tmem_wait_ld(s1);
-          add(s0, 0);
-          add(s1, 1);
-          tmem_ld32(scol + 64, s0);
-          tmem_ld32(scol + 96, s1);
-          tmem_wait_ld(s0);
-          tmem_wait_ld(s1);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.s_empty[kt][it % 3]);
-        if (look != 0) {
-          add(s0, 2);
-          add(s1, 3);
-          float a[8];
+        uint32_t s0[16], s1[16];
+        const uint32_t scol = tbase + lane_off + C::kColS + (uint32_t)(buf * kTile + half * 64);
+        if constexpr (!kMask) {
+          if (has_keys) {
+            tmem_ld16(scol, s0);
+            tmem_wait_ld16(s0);
+            tmem_ld16(scol + 16, s1);
+            add(s0, 0, false, 0u);
+            tmem_wait_ld16(s1);
+            tmem_ld16(scol + 32, s0);
+            add(s1, 1, false, 0u);
+            tmem_wait_ld16(s0);
+            tmem_ld16(scol + 48, s1);
+            add(s0, 2, false, 0u);
+            tmem_wait_ld16(s1);
+          }
+          tc_fence_before();
+          mbar_arrive(&g.s_empty[kt]);
+          if (has_keys) add(s1, 3, false, 0u);
+        } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) u2f(acc[k], a[2 * k], a[2 * k + 1]);
-          total += ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+          for (int c = 0; c < 2; ++c) {
+            // a query that saw nothing adds nothing, whatever its row holds
+            uint32_t w = g.nl[half * 64 + c * 32 + lane] == -INFINITY ? 0u : seen[c];
+            // no sum is kept for the keys past the slot's end: as good as seen
+            const int past = p.T - (key - lane);
+            const uint32_t all = past < 32 && past > 0 ? w | (~0u << past) : w;
+            if (!__any_sync(0xffffffffu, w != 0u)) continue;
+            tmem_ld16(scol + c * 32, s0);
+            tmem_wait_ld16(s0);
+            tmem_ld16(scol + c * 32 + 16, s1);
+            if (__all_sync(0xffffffffu, all == ~0u)) {
+              add(s0, 2 * c, false, 0u);
+              tmem_wait_ld16(s1);
+              add(s1, 2 * c + 1, false, 0u);
+            } else {
+              // a bit a query for this lane's key: the 32 x 32 bits transposed
+#pragma unroll
+              for (int j = 16; j > 0; j >>= 1) {
+                const uint32_t m = j == 16 ? 0x0000FFFFu : j == 8 ? 0x00FF00FFu : j == 4 ? 0x0F0F0F0Fu
+                                                        : j == 2  ? 0x33333333u
+                                                                  : 0x55555555u;
+                const uint32_t y = __shfl_xor_sync(0xffffffffu, w, j);
+                w = (lane & j) ? (w & ~m) | ((y >> j) & m) : (w & m) | ((y & m) << j);
+              }
+              add(s0, 2 * c, true, w);
+              tmem_wait_ld16(s1);
+              add(s1, 2 * c + 1, true, w >> 16);
+            }
+          }
+          tc_fence_before();
+          mbar_arrive(&g.s_empty[kt]);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.q_empty[st]);
+        const uint64_t a = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+        float lo, hi;
+        u2f(a, lo, hi);
+        total += lo + hi;
+        mbar_arrive(&g.l_empty);
         buf = buf == 0 ? 2 : buf - 1;  // two steps on, modulo 3
-        ++it;
+        it.step();
       }
       if (!ok) break;
-      if (ns == 1) {
-        if (mine) p.out[at] = __fmaf_rn(p.decay, before, total);
+      // the second half's sums to the first
+      if (half == 1) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars.t_empty[kt], ((uint32_t)done & 1u) ^ 1u, &abort_flag, tmo));
+        if (!ok) break;
+        half_sum[kt][row] = total;
+        mbar_arrive(&bars.t_full[kt]);
       } else {
-        st_cluster_f32(mapa_shared(smem_u32(&part[rank][kt * kTile + row]), 0), total);
-        __syncwarp();
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars.t_full[kt], (uint32_t)done & 1u, &abort_flag, tmo));
+        if (!ok) break;
+        total += half_sum[kt][row];
+        mbar_arrive(&bars.t_empty[kt]);
+        if (ns == 1) {
+          if (mine) p.out[at] = __fmaf_rn(p.decay, before, total);
+        } else {
+          st_cluster_f32(mapa_shared(smem_u32(&part[rank][kt * kTile + row]), 0), total);
+          __syncwarp();
+        }
       }
+      ++done;
     }
     if (!ok) {
       if (lane == 0) {
@@ -570,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   __syncwarp();
   if (ns > 1) {
     cluster_sync();  // the partial sums are there
-    if (rank == 0 && warp >= 4 && part_lost == 0.0f) {
+    if (rank == 0 && warp >= 4 && warp < 12 && part_lost == 0.0f) {
       const Unit un = unit_of(p, u0);
       const int j = threadIdx.x - 128;
       const int key = un.kp * 2 * kTile + j;
@@ -594,9 +696,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     const int zero = 0;
     if (warp == 0 && lane == 0) {
       if (k_issued > 0) mbar_wait(&bars.k_full, (uint32_t)(k_issued - 1) & 1u, &zero, tmo);
-      for (int i = (q_issued > kStages ? q_issued - kStages : 0); i < q_issued; ++i) {
+      for (int i = (q_issued > C::kStages ? q_issued - C::kStages : 0); i < q_issued; ++i) {
         if (p.fault_mode == 2 && i == 1) continue;  // the copy the test hook withheld
-        mbar_wait(&bars.q_full[i % kStages], (uint32_t)(i / kStages) & 1u, &zero, tmo);
+        mbar_wait(&bars.q_full[i % C::kStages], (uint32_t)(i / C::kStages) & 1u, &zero, tmo);
       }
     } else if (warp == 1 || warp == 3) {
       mma_commit_warp(&bars.drain);  // the same elected lane that issued the MMAs

@@ -34,6 +34,9 @@ struct alignas(128) WeightParams {
   const uint32_t* hist_mask;
   int32_t hist_states;
   int32_t hist_words;
+  // Key tiles that the token masks leave anything of, as in AttnParams, or null
+  const uint8_t* any_tile;
+  int32_t any_stride;
   int32_t masked;       // some mask, or a frame-causal node
   // The distinct slots that the nodes see, those seen by most nodes first, and
   // for slot i the nodes that see it: refs [first[i], first[i + 1]).
