@@ -147,19 +147,19 @@ __device__ __forceinline__ float ld_f32_if(const float* p, bool load, float othe
 template <bool kMask>
 struct Walk {
   const uint32_t* marks;
-  int at, end, n_qt, r, qt;
-  uint32_t left;
+  int at, end, n_qt, r, qt;  // kMask: word of the bitmap, and the first item of ref r in `qt`
+  uint32_t left;             // kMask: the word's bits still to come
   __device__ __forceinline__ Walk(const uint32_t* marks_, int begin, int end_, int n_qt_)
       : marks(marks_), at(begin), end(end_), n_qt(n_qt_), r(begin > 0 ? begin / n_qt_ : 0), qt(begin - r * n_qt_), left(0) {
     if constexpr (kMask) {
       left = begin < end ? marks[begin >> 5] & (~0u << (begin & 31)) : 0u;
       at = begin >> 5;
+      qt = r * n_qt;
     }
   }
   // How many there are (before the first next).
   __device__ __forceinline__ int count() const {
     if constexpr (kMask) {
-      if (at * 32 >= end) return 0;
       int n = 0;
       const int words = (end + 31) >> 5;
       for (int w = at; w < words; ++w) {
@@ -183,8 +183,12 @@ struct Walk {
       const int i = (at << 5) + __ffs(left) - 1;
       left &= left - 1u;
       if (i >= end) return false;
-      r_out = i / n_qt;
-      qt_out = i - r_out * n_qt;
+      while (i - qt >= n_qt) {
+        qt += n_qt;
+        ++r;
+      }
+      r_out = r;
+      qt_out = i - qt;
       return true;
     } else {
       if (at >= end) return false;
@@ -254,10 +258,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     }
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&stage[s].l_full, 1);
-      mbar_init(&stage[s].l_empty, 2 * kGroupWarps * 32);
+      mbar_init(&stage[s].l_empty, 2 * kGroupWarps);
       for (int k = 0; k < 2; ++k) {
         mbar_init(&stage[s].s_full[k], 1);
-        mbar_init(&stage[s].s_empty[k], kGroupWarps * 32);
+        mbar_init(&stage[s].s_empty[k], kGroupWarps);
       }
     }
     mbar_init(&bars.k_full, 1);
@@ -582,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         uint32_t s0[16], s1[16];
         const uint32_t scol = tbase + lane_off + C::kColS + (uint32_t)(buf * kTile + half * 64);
         if constexpr (!kMask) {
-          if (has_keys) {
+          {
             tmem_ld16(scol, s0);
             tmem_wait_ld16(s0);
             tmem_ld16(scol + 16, s1);
@@ -596,8 +600,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
             tmem_wait_ld16(s1);
           }
           tc_fence_before();
-          mbar_arrive(&g.s_empty[kt]);
-          if (has_keys) add(s1, 3, false, 0u);
+          __syncwarp(); if (lane == 0) mbar_arrive(&g.s_empty[kt]);
+          add(s1, 3, false, 0u);
         } else {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -630,13 +634,13 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
             }
           }
           tc_fence_before();
-          mbar_arrive(&g.s_empty[kt]);
+          __syncwarp(); if (lane == 0) mbar_arrive(&g.s_empty[kt]);
         }
         const uint64_t a = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
         float lo, hi;
         u2f(a, lo, hi);
         total += lo + hi;
-        mbar_arrive(&g.l_empty);
+        __syncwarp(); if (lane == 0) mbar_arrive(&g.l_empty);
         buf = buf == 0 ? 2 : buf - 1;  // two steps on, modulo 3
         it.step();
       }
