@@ -4,13 +4,18 @@
 //
 // Two launches.  condense_select_kernel finds which: a cluster of up to eight
 // CTAs per head, each with a contiguous range of the head's candidates in shared
-// memory as ordered integer keys, finds the T-th largest key digit by digit (11,
-// 11 and 10 bits: a histogram of the candidates that match the digits so far,
-// summed over the cluster through distributed shared memory, each CTA picking
-// the digit for itself), then ranks what is kept: everything above that key, and
-// of those equal to it the first ones in candidate order.  Counts and ranks are
-// integers, so the result does not depend on the order of the atomics.
+// memory, finds the T-th largest key (the weights as integers of the same order)
+// digit by digit, 11, 11 and 10 bits.  The first digit's histogram has few bins in
+// use; each CTA adds its own to every CTA's sums through distributed shared
+// memory, and each finds the digit for itself.  The candidates with that digit are
+// then few and gathered by every CTA, which finds the other digits alone (a cluster
+// barrier costs 0.7 us, reading eight histograms of 2048 bins 1.5 to 2 us); or all
+// equal (tokens that nothing attended); or the other digits are found like the
+// first, each CTA reading all histograms.  Then what stays is ranked: everything
+// above the key, and of the candidates equal to it the first ones.  Counts and ranks
+// are integers, so the result does not depend on the order of the atomics.
 // condense_gather_kernel then copies the kept rows of K and V: bound by HBM.
+#include <algorithm>
 #include <mutex>
 
 #include <cuda_runtime.h>
@@ -21,125 +26,277 @@
 namespace sva {
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 512;
+constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kBins = 2048;
-// Keys that a CTA holds in shared memory; a longer range is read again for each
+constexpr int kBinsPerThread = kBins / kSelThreads;
+static_assert(kBinsPerThread == 4, "a thread takes a vector of bins");
+// Weights that a CTA holds in shared memory; a longer range is read again for each
 // digit.
-constexpr int kHeldKeys = 48 * 1024;
+constexpr int kHeldKeys = 40 * 1024;
+// Candidates that share the first digit with the line, up to this many in all
+// CTAs, are gathered by every CTA of the cluster.
+constexpr int kListKeys = 4096;
 
-// Weights as integers of the same order; NaN counts as -inf, -0 as 0.
-__device__ __forceinline__ uint32_t key_of(float w) {
+// Weights (their bits) as integers of the same order; NaN counts as -inf, -0 as 0.
+__device__ __forceinline__ uint32_t key_of(uint32_t bits) {
+  float w = __uint_as_float(bits);
   if (w != w) w = -INFINITY;
   const uint32_t u = __float_as_uint(w + 0.0f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t cluster_addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(cluster_addr));
   return v;
 }
 
-// Exclusive sum over the block of a pair of counts, in thread order; `all` is the
-// sum of all.  Every thread calls it.
-__device__ __forceinline__ uint2 block_scan(uint2 v, uint2* warp_sum, uint2* all) {
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr));
+  return v;
+}
+
+__device__ __forceinline__ void add_cluster_u32(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
+// The halves of a cluster barrier.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Exclusive sum over the block, in thread order; `all`: the sum of all.  Two
+// counts of up to 2^31 in one 64-bit sum.  Every thread calls it.
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* warp_sum, uint64_t* all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint2 s = v;
+  uint64_t s = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, s.x, o), b = __shfl_up_sync(0xffffffffu, s.y, o);
-    if (lane >= o) {
-      s.x += a;
-      s.y += b;
-    }
+    const uint64_t a = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += a;
   }
   if (lane == 31) warp_sum[warp] = s;
   __syncthreads();
-  uint2 w = warp_sum[lane];  // 32 warps: every warp sums all of them
+  uint64_t w = lane < kSelWarps ? warp_sum[lane] : 0;  // every warp sums all of them
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, w.x, o), b = __shfl_up_sync(0xffffffffu, w.y, o);
-    if (lane >= o) {
-      w.x += a;
-      w.y += b;
-    }
+  for (int o = 1; o < kSelWarps; o <<= 1) {
+    const uint64_t a = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += a;
   }
-  all->x = __shfl_sync(0xffffffffu, w.x, 31);
-  all->y = __shfl_sync(0xffffffffu, w.y, 31);
-  const uint32_t bx = __shfl_sync(0xffffffffu, w.x, warp > 0 ? warp - 1 : 0);
-  const uint32_t by = __shfl_sync(0xffffffffu, w.y, warp > 0 ? warp - 1 : 0);
-  __syncthreads();  // warp_sum may be written again
-  return make_uint2(s.x - v.x + (warp > 0 ? bx : 0u), s.y - v.y + (warp > 0 ? by : 0u));
+  *all = __shfl_sync(0xffffffffu, w, kSelWarps - 1);
+  const uint64_t before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+  return s - v + (warp > 0 ? before : 0);
 }
 
-__global__ void __launch_bounds__(kSelThreads, 1) condense_select_kernel(const __grid_constant__ CondenseParams p) {
-  extern __shared__ uint32_t held[];
-  __shared__ uint32_t hist[2][kBins];  // of two digits in turn
-  __shared__ uint2 warp_sum[32];
-  __shared__ uint32_t digit_sh, above_sh;
-  __shared__ uint2 count_sh;           // this CTA's candidates above the line and on it
-  const int tid = threadIdx.x;
-  const int nc = p.cluster;
-  const int h = (int)blockIdx.x / nc, rank = (int)blockIdx.x - h * nc;
+// The digit of a histogram (four bins a thread in `bins`, thread 0 the largest)
+// at which the count from the top reaches `need`.
+struct Digit {
+  uint32_t digit, above, here;  // candidates above the digit, and with it
+};
+__device__ __forceinline__ Digit find_digit(uint4 bins, int need, uint64_t* warp_sum, Digit* found) {
+  uint64_t all;
+  const uint32_t total = bins.x + bins.y + bins.z + bins.w;
+  uint32_t at = (uint32_t)block_scan(total, warp_sum, &all);
+  const uint32_t line = (uint32_t)need;
+  if (at < line && at + total >= line) {
+    uint32_t digit = (uint32_t)(kBins - 1 - 4 * threadIdx.x), here = bins.w;
+    if (at + here < line) {
+      at += here;
+      --digit;
+      here = bins.z;
+      if (at + here < line) {
+        at += here;
+        --digit;
+        here = bins.y;
+        if (at + here < line) {
+          at += here;
+          --digit;
+          here = bins.x;
+        }
+      }
+    }
+    *found = {digit, at, here};
+  }
+  __syncthreads();
+  return *found;
+}
+
+// kCluster CTAs a head.
+template <int kCluster>
+__global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const __grid_constant__ CondenseParams p) {
+  extern __shared__ uint32_t held[];               // the range's weights, then this CTA's list
+  __shared__ alignas(16) uint32_t hist[2][kBins];  // of this CTA's candidates
+  __shared__ alignas(16) uint32_t sums[kBins];     // the first digit's, of the cluster
+  __shared__ uint32_t list[kListKeys];             // the cluster's candidates with the first digit
+  __shared__ uint64_t warp_sum[6][kSelWarps];      // of each scan
+  __shared__ Digit found[5];
+  __shared__ alignas(16) uint32_t match_sh[4];     // this CTA's candidates with the first digit: how many, least, largest
+  __shared__ alignas(16) uint32_t count_sh[4];     // this CTA's candidates above the line and on it
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int h = (int)blockIdx.x / kCluster, rank = (int)blockIdx.x - h * kCluster;
   const int n = p.n_src * p.T;
-  const int per = (n + nc - 1) / nc;
+  const int per = (n + kCluster - 1) / kCluster;
   const int e0 = min(rank * per, n), count = min(per, n - e0);
   const bool hold = p.hold != 0;
+  uint32_t* mine = held + (hold ? per : 0);
+  const int b0 = kBins - 4 - 4 * tid;              // this thread's bins
+  const uint4 zero = make_uint4(0, 0, 0, 0);
 
   ptx::pdl_launch_dependents();
-  for (int b = tid; b < kBins; b += kSelThreads) hist[0][b] = 0;
+  *reinterpret_cast<uint4*>(&hist[0][tid * 4]) = zero;
+  *reinterpret_cast<uint4*>(&hist[1][tid * 4]) = zero;
+  *reinterpret_cast<uint4*>(&sums[tid * 4]) = zero;
+  if (tid == 0) {
+    match_sh[0] = 0;
+    match_sh[1] = ~0u;
+    match_sh[2] = 0;
+  }
+  __syncwarp();
+  if constexpr (kCluster > 1) cluster_arrive();    // the sums are clear
   ptx::pdl_wait();
+  const uint32_t* weight = reinterpret_cast<const uint32_t*>(p.weight);
   auto load = [&](int e) {  // candidate e of the head
     const int i = e / p.T;
-    return p.weight + ((size_t)p.slot[i] * p.H + h) * p.T + (e - i * p.T);
+    return weight[((size_t)p.slot[i] * p.H + h) * p.T + (e - i * p.T)];
   };
-  auto key_at = [&](int j) { return hold ? held[j] : key_of(*load(e0 + j)); };
+  auto bits_at = [&](int j) { return hold ? held[j] : load(e0 + j); };
   __syncthreads();
 
-  uint32_t prefix = 0;   // the digits found so far
-  int need = p.T;        // of the candidates that match them, the ones to keep
-  int shift = 32;
+  // First digit: the few bins in use are added to every CTA's sums.
+#pragma unroll 4
+  for (int j = tid; j < count; j += kSelThreads) {
+    const uint32_t w = load(e0 + j);
+    if (hold) held[j] = w;
+    atomicAdd(&hist[0][key_of(w) >> 21], 1u);
+  }
+  __syncthreads();
+  if constexpr (kCluster > 1) {
+    cluster_wait();
+#pragma unroll
+    for (int k = 0; k < kBinsPerThread; ++k) {
+      const int b = tid + k * kSelThreads;
+      const uint32_t v = hist[0][b];
+      if (v != 0)
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) add_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&sums[b]), (uint32_t)c), v);
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
+  const uint32_t* first = kCluster > 1 ? sums : hist[0];
+  Digit d = find_digit(*reinterpret_cast<const uint4*>(&first[b0]), p.T, warp_sum[0], &found[0]);
+  uint32_t prefix = d.digit << 21;   // the digits found so far
+  int need = p.T - (int)d.above;     // of the candidates that match them, the ones to keep
+  const bool listed = d.here <= (uint32_t)kListKeys;
+
+  // The candidates that match: their keys where they are few, their range.
+  uint32_t least = ~0u, most = 0;
+  for (int j = tid; j < count; j += kSelThreads) {
+    const uint32_t k = key_of(bits_at(j));
+    if (((k ^ prefix) >> 21) != 0u) continue;
+    least = min(least, k);
+    most = max(most, k);
+    if (listed) mine[atomicAdd(&match_sh[0], 1u)] = k;
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0 && least <= most) {
+    atomicMin(&match_sh[1], least);
+    atomicMax(&match_sh[2], most);
+  }
+  uint4 match[kCluster];
+  if constexpr (kCluster > 1) {
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+#pragma unroll
+    for (int c = 0; c < kCluster; ++c)
+      match[c] = ld_cluster_v4(ptx::mapa_shared(ptx::smem_u32(match_sh), (uint32_t)c));
+  } else {
+    __syncthreads();
+    match[0] = *reinterpret_cast<const uint4*>(match_sh);
+  }
+  least = ~0u;
+  most = 0;
+#pragma unroll
+  for (int c = 0; c < kCluster; ++c) {
+    least = min(least, match[c].y);
+    most = max(most, match[c].z);
+  }
+  if (least == most) {  // all of them equal (tokens that nothing attended)
+    prefix = least;
+  } else if (listed) {
+    // Every CTA gathers the cluster's and finds the other digits for itself.
+    const uint32_t* keys = mine;
+    if constexpr (kCluster > 1) {
+      uint32_t at = 0;
+#pragma unroll
+      for (int c = 0; c < kCluster; ++c) {
+        for (uint32_t j = tid; j < match[c].x; j += kSelThreads)
+          list[at + j] = ld_cluster_u32(ptx::mapa_shared(ptx::smem_u32(mine + j), (uint32_t)c));
+        at += match[c].x;
+      }
+      keys = list;
+      __syncthreads();
+    }
+    const uint32_t m = d.here;
+    *reinterpret_cast<uint4*>(&hist[0][tid * 4]) = zero;
+    for (uint32_t j = tid; j < m; j += kSelThreads) atomicAdd(&hist[1][(keys[j] >> 10) & 2047u], 1u);
+    __syncthreads();
+    d = find_digit(*reinterpret_cast<const uint4*>(&hist[1][b0]), need, warp_sum[1], &found[1]);
+    prefix |= d.digit << 10;
+    need -= (int)d.above;
+    for (uint32_t j = tid; j < m; j += kSelThreads) {
+      const uint32_t k = keys[j];
+      if (((k ^ prefix) >> 10) == 0u) atomicAdd(&hist[0][k & 1023u], 1u);
+    }
+    __syncthreads();
+    d = find_digit(*reinterpret_cast<const uint4*>(&hist[0][b0]), need, warp_sum[2], &found[2]);
+    prefix |= d.digit;
+    need -= (int)d.above;
+  } else {
+    // The cluster's histogram of each digit, by every CTA.
+    *reinterpret_cast<uint4*>(&hist[0][tid * 4]) = zero;
 #pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int bits = pass < 2 ? 11 : 10;
-    const uint32_t mask = pass == 0 ? 0u : ~0u << shift;
-    shift -= bits;
-    uint32_t* hs = hist[pass & 1];
-    for (int j = tid; j < count; j += kSelThreads) {
-      uint32_t k;
-      if (pass == 0) {
-        k = key_of(*load(e0 + j));
-        if (hold) held[j] = k;
+    for (int pass = 1; pass < 3; ++pass) {
+      const int shift = pass == 1 ? 10 : 0;
+      uint32_t* hs = hist[pass & 1];
+      for (int j = tid; j < count; j += kSelThreads) {
+        const uint32_t k = key_of(bits_at(j));
+        if (((k ^ prefix) >> (pass == 1 ? 21 : 10)) == 0u) atomicAdd(&hs[(k >> shift) & (pass == 1 ? 2047u : 1023u)], 1u);
+      }
+      uint4 bins = zero;
+      if constexpr (kCluster > 1) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        uint4 part[kCluster];
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c)
+          part[c] = ld_cluster_v4(ptx::mapa_shared(ptx::smem_u32(&hs[b0]), (uint32_t)c));
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) {
+          bins.x += part[c].x;
+          bins.y += part[c].y;
+          bins.z += part[c].z;
+          bins.w += part[c].w;
+        }
       } else {
-        k = key_at(j);
+        __syncthreads();
+        bins = *reinterpret_cast<const uint4*>(&hs[b0]);
       }
-      if (((k ^ prefix) & mask) == 0u) atomicAdd(&hs[(k >> shift) & ((1u << bits) - 1u)], 1u);
+      d = find_digit(bins, need, warp_sum[2 + pass], &found[2 + pass]);
+      prefix |= d.digit << shift;
+      need -= (int)d.above;
     }
-    __syncthreads();
-    if (nc > 1) ptx::cluster_sync();
-    // two bins a thread, the largest digits first
-    uint2 mine = make_uint2(0u, 0u);
-    const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
-    if (nc > 1) {
-      for (int c = 0; c < nc; ++c) {
-        mine.x += ld_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&hs[b1]), c));
-        mine.y += ld_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&hs[b0]), c));
-      }
-    } else {
-      mine = make_uint2(hs[b1], hs[b0]);
-    }
-    // the other histogram was last read before this pass's cluster barrier
-    for (int b = tid; b < kBins; b += kSelThreads) hist[(pass + 1) & 1][b] = 0;
-    uint2 all;
-    const uint32_t before = block_scan(make_uint2(mine.x + mine.y, 0u), warp_sum, &all).x;
-    if (before < (uint32_t)need && before + mine.x + mine.y >= (uint32_t)need) {
-      const bool first = before + mine.x >= (uint32_t)need;
-      digit_sh = (uint32_t)(first ? b1 : b0);
-      above_sh = before + (first ? 0u : mine.x);
-    }
-    __syncthreads();
-    prefix |= digit_sh << shift;
-    need -= (int)above_sh;
   }
 
   // `need` (>= 1) of the candidates equal to `prefix` stay, and all above it.  A
@@ -147,41 +304,53 @@ __global__ void __launch_bounds__(kSelThreads, 1) condense_select_kernel(const _
   // warp on one bank).
   const int run = ((count + kSelThreads - 1) / kSelThreads) | 1;
   const int j0 = min(tid * run, count), j1 = min(j0 + run, count);
-  uint2 my = make_uint2(0u, 0u);
+  uint32_t above = 0, equal = 0;
   for (int j = j0; j < j1; ++j) {
-    const uint32_t k = key_at(j);
-    my.x += k > prefix;
-    my.y += k == prefix;
+    const uint32_t k = key_of(bits_at(j));
+    above += k > prefix;
+    equal += k == prefix;
   }
-  uint2 all;
-  uint2 at = block_scan(my, warp_sum, &all);
+  uint64_t all;
+  const uint64_t at = block_scan((uint64_t)above << 32 | equal, warp_sum[5], &all);
   int kept = 0, level = 0;  // kept and equal candidates of the CTAs before this one
-  if (nc > 1) {
-    if (tid == 0) count_sh = all;
-    ptx::cluster_sync();
-    for (int c = 0; c < rank; ++c) {
-      const uint32_t a = ptx::mapa_shared(ptx::smem_u32(&count_sh), c);
-      kept += (int)ld_cluster_u32(a);
-      level += (int)ld_cluster_u32(a + 4);
+  if constexpr (kCluster > 1) {
+    if (tid == 0) {
+      count_sh[0] = (uint32_t)(all >> 32);
+      count_sh[1] = (uint32_t)all;
     }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    uint4 part[kCluster];
+#pragma unroll
+    for (int c = 0; c < kCluster; ++c) part[c] = ld_cluster_v4(ptx::mapa_shared(ptx::smem_u32(count_sh), (uint32_t)c));
+#pragma unroll
+    for (int c = 0; c < kCluster; ++c) {
+      kept += c < rank ? (int)part[c].x : 0;
+      level += c < rank ? (int)part[c].y : 0;
+    }
+    __syncwarp();
+    cluster_arrive();  // no CTA leaves while another may still read its counts
     kept += min(level, need);
   }
-  int eq = level + (int)at.y;                               // equal ones before this thread's
-  int out = kept + (int)at.x + min(eq, need) - min(level, need);
+  int eq = level + (int)(uint32_t)at;                       // equal ones before this thread's
+  int out = kept + (int)(at >> 32) + min(eq, need) - min(level, need);
   int32_t* index = p.index + (size_t)h * p.T;
-  float* weight = p.weight + ((size_t)p.dst * p.H + h) * p.T;
+  uint32_t* kept_weight = reinterpret_cast<uint32_t*>(p.weight) + ((size_t)p.dst * p.H + h) * p.T;
   for (int j = j0; j < j1; ++j) {
-    const uint32_t k = key_at(j);
+    const uint32_t w = bits_at(j), k = key_of(w);
     const bool same = k == prefix;
     if (k > prefix || (same && eq < need)) {
       index[out] = e0 + j;
-      weight[out] = *load(e0 + j);
+      kept_weight[out] = w;
       ++out;
     }
     eq += same;
   }
-  // no CTA leaves while another may still read its counts
-  if (nc > 1) ptx::cluster_sync();
+  if constexpr (kCluster > 1) {
+    __syncwarp();
+    cluster_wait();
+  }
 }
 
 // K and V rows of the kept candidates, kRows rows a thread group in flight.
@@ -224,7 +393,10 @@ __global__ void __launch_bounds__(256) condense_gather_kernel(const __grid_const
 
 }  // namespace
 
-cudaError_t launch_condense(CondenseParams& p, cudaStream_t s) {
+cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s) {
+  using Kernel = void (*)(const CondenseParams);
+  static const Kernel select[4] = {condense_select_kernel<1>, condense_select_kernel<2>, condense_select_kernel<4>,
+                                   condense_select_kernel<8>};
   static std::mutex mu;
   static bool configured[64] = {};
   int dev = 0;
@@ -234,19 +406,24 @@ cudaError_t launch_condense(CondenseParams& p, cudaStream_t s) {
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!configured[dev]) {
-      e = cudaFuncSetAttribute(condense_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               kHeldKeys * 4);
-      if (e != cudaSuccess) return e;
+      for (Kernel k : select) {
+        e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (kHeldKeys + kListKeys) * 4);
+        if (e != cudaSuccess) return e;
+      }
       configured[dev] = true;
     }
   }
   const int n = p.n_src * p.T;
-  p.cluster = n <= 4096 ? 1 : (n <= 8192 ? 2 : (n <= 16384 ? 4 : 8));
-  const int per = (n + p.cluster - 1) / p.cluster;
+  // About 2048 candidates a CTA, at most eight CTAs a head, and no more of them than
+  // run at once (two an SM).
+  int log2_cluster = 0;
+  while (log2_cluster < 3 && n > 2048 << log2_cluster && (long long)p.H << (log2_cluster + 1) <= 2ll * num_sms)
+    ++log2_cluster;
+  const int per = (n + (1 << log2_cluster) - 1) >> log2_cluster;
   p.hold = per <= kHeldKeys ? 1 : 0;
-  LaunchConfig sel(dim3((unsigned)(p.H * p.cluster)), kSelThreads, p.hold ? (size_t)per * 4 : 0, s,
-                   p.cluster > 1 ? p.cluster : 0);
-  e = cudaLaunchKernelEx(&sel.cfg, condense_select_kernel, p);
+  LaunchConfig sel(dim3((unsigned)(p.H << log2_cluster)), kSelThreads, (size_t)((p.hold ? per : 0) + std::min(per, kListKeys)) * 4, s,
+                   log2_cluster > 0 ? 1 << log2_cluster : 0);
+  e = cudaLaunchKernelEx(&sel.cfg, select[log2_cluster], p);
   if (e != cudaSuccess) return e;
   const int rows = 256 / (p.d >> 3) * kRows;
   LaunchConfig copy(dim3((unsigned)((p.T + rows - 1) / rows), (unsigned)p.H), 256, 0, s);

@@ -11,12 +11,11 @@ struct CondenseParams {
   void* pool;       // slot pool base, bf16 [num_slots][2][H][Tpad][d]
   int32_t T, Tpad, H, d;
   int32_t n_src, dst;
-  int32_t cluster;  // CTAs per head of the selection
   int32_t hold;     // 1: a CTA's keys stay in shared memory
   int32_t slot[SVA_MAX_CTX];
 };
 
-// Sets p.cluster and p.hold.
-cudaError_t launch_condense(CondenseParams& p, cudaStream_t s);
+// Sets p.hold.
+cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s);
 
 }  // namespace sva

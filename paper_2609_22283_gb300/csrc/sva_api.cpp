@@ -1453,7 +1453,7 @@ sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_s
   p.d = g.head_dim;
   p.n_src = n_src;
   p.dst = dst_slot;
-  cudaError_t e = sva::launch_condense(p, reinterpret_cast<cudaStream_t>(s));
+  cudaError_t e = sva::launch_condense(p, c->num_sms, reinterpret_cast<cudaStream_t>(s));
   if (e != cudaSuccess) return cuda_fail(e, "condense launch");
   c->slots[dst_slot].resident = true;
   return ok();
