@@ -111,10 +111,6 @@ struct RopeParams {
   RopeNode nodes[SVA_MAX_NODES];
 };
 
-// Norm weights of sva_rope_kv_write_headnorm: none, one [d] vector for every
-// head, or [H][d].
-enum class HeadGamma { kNone, kShared, kHeads };
-
 struct RopeHeadParams {
   const void* k;  // bf16, token t (of all nodes') at t * k_stride elements, [H][d] each
   const void* v;
@@ -125,9 +121,9 @@ struct RopeHeadParams {
   const float2* tab_t;  // rotation tables, as in RopeParams
   const float2* tab_h;
   const float2* tab_w;
-  const float* gamma_k;
+  const float* gamma_k;  // null: ones
   const float* gamma_q;
-  HeadGamma gamma;
+  int32_t gamma_heads;   // 1: one [d] vector for every head; else [H][d]
   float eps;
   int32_t T, H, d, Tpad, Hp, Wp, P0, P1, P2;
   int32_t n_nodes;

@@ -7,6 +7,8 @@
 // whole H*d vector, a row's sum of squares stays inside d / 8 lanes, so no warp
 // waits for another and a token's heads can be spread over as many warps as a
 // launch needs to fill the GPU.
+#include <algorithm>
+
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -66,8 +68,19 @@ __device__ __forceinline__ uint4 norm_turn(uint4 v, const Gamma8& g, const float
 // heads have fewer vectors) walk kBatch vectors each of one token's rows, `group`
 // apart, all their loads issued before the first store.  `group` is a multiple of
 // the d / 8 vectors of a row, so a lane holds the same four pairs in every vector.
-template <int kBatch, bool kQ, HeadGamma kGamma>
-__global__ void __launch_bounds__(256, kBatch <= 2 ? 4 : 2) rope_head_kernel(const __grid_constant__ RopeHeadParams p) {
+//
+// Bound by HBM.  Four blocks of eight warps an SM with two vectors a lane keep 98 KB
+// of loads in flight an SM; held to 64 registers, so a row's gammas are fetched where
+// they are used (from L1), K's before Q's: with both at hand the instances with Q
+// spill (18720 tokens of 12 x 128 with Q, gammas a head 61.4 us, 57.0 so; 4680 of 40
+// x 128 52.0 and 48.2).  Three vectors at three blocks: 58.1 and 50.0.  The grid is
+// at most eight blocks an SM: a block that loops has its gammas and tables in L1 (4680
+// tokens of 12 x 128, K and V, 12.3 us, 13.0 at sixteen, 13.0 with a block a part).
+// Times with three sets of buffers in a graph: one 4680-token node of 12 x 128 with Q
+// 17.3 us (86 MB, 5.0 TB/s; a device copy of its 43 MB takes 20.5 us in such a loop),
+// four 57.0 us (6.1 TB/s), K and V of 40 x 128 32.9 us (5.8 TB/s).
+template <int kBatch, bool kQ, bool kGamma>
+__global__ void __launch_bounds__(256, 4) rope_head_kernel(const __grid_constant__ RopeHeadParams p) {
   const int lane = threadIdx.x & 31;
   const int vpr = p.d >> 3;                      // 16-byte vectors of a row
   const int vshift = vpr == 16 ? 4 : 3;
@@ -84,11 +97,6 @@ __global__ void __launch_bounds__(256, kBatch <= 2 ? 4 : 2) rope_head_kernel(con
   __nv_bfloat16* qout = static_cast<__nv_bfloat16*>(p.q_out);
   __nv_bfloat16* cache = static_cast<__nv_bfloat16*>(p.cache);
   ptx::pdl_wait();
-  Gamma8 gk{}, gq{};
-  if constexpr (kGamma == HeadGamma::kShared) {
-    gk = gamma_at(p.gamma_k + c8 * 8);
-    if constexpr (kQ) gq = gamma_at(p.gamma_q + c8 * 8);
-  }
   const int per_warp = 32 / p.group;
   const int units = (p.n_nodes * p.T * p.parts + per_warp - 1) / per_warp;  // of a warp
   const int warps = gridDim.x * (blockDim.x >> 5);
@@ -135,14 +143,16 @@ __global__ void __launch_bounds__(256, kBatch <= 2 ? 4 : 2) rope_head_kernel(con
     for (int j = 0; j < kBatch; ++j) {
       const int v = v0 + j * p.group;
       const bool in = v < per_tok;
-      if constexpr (kGamma == HeadGamma::kHeads) {
-        if (in) gk = gamma_at(p.gamma_k + v * 8);
-        if (kQ && in) gq = gamma_at(p.gamma_q + v * 8);
-      }
+      const int gv = p.gamma_heads > 1 ? v * 8 : c8 * 8;
+      Gamma8 g{};
+      if (kGamma && in) g = gamma_at(p.gamma_k + gv);
       // the shuffles inside want every lane, in range or not
-      const uint4 k = norm_turn<kGamma != HeadGamma::kNone>(kv[j], gk, cs, vpr, inv_d, p.eps);
+      const uint4 k = norm_turn<kGamma>(kv[j], g, cs, vpr, inv_d, p.eps);
       uint4 q{};
-      if constexpr (kQ) q = norm_turn<kGamma != HeadGamma::kNone>(qv[j], gq, cs, vpr, inv_d, p.eps);
+      if constexpr (kQ) {
+        if (kGamma && in) g = gamma_at(p.gamma_q + gv);
+        q = norm_turn<kGamma>(qv[j], g, cs, vpr, inv_d, p.eps);
+      }
       if (in) {
         __nv_bfloat16* dst = out + (size_t)(v >> vshift) * p.Tpad * p.d;
         *reinterpret_cast<uint4*>(dst) = k;
@@ -153,26 +163,18 @@ __global__ void __launch_bounds__(256, kBatch <= 2 ? 4 : 2) rope_head_kernel(con
   }
 }
 
-template <int kBatch, bool kQ>
-cudaError_t launch_gamma(const RopeHeadParams& p, const LaunchConfig& l) {
-  switch (p.gamma) {
-    case HeadGamma::kNone:
-      return cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, kQ, HeadGamma::kNone>, p);
-    case HeadGamma::kShared:
-      return cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, kQ, HeadGamma::kShared>, p);
-    default:
-      return cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, kQ, HeadGamma::kHeads>, p);
-  }
-}
-
 template <int kBatch>
 cudaError_t launch_batch(RopeHeadParams& p, int num_sms, cudaStream_t s) {
   const int per_tok = p.H * (p.d >> 3);
   p.parts = (per_tok + p.group * kBatch - 1) / (p.group * kBatch);
   const long long units = ((long long)p.n_nodes * p.T * p.parts * p.group + 31) / 32;
-  const long long blocks = (units + 7) / 8;
-  LaunchConfig l(dim3((unsigned)(blocks < 16ll * num_sms ? blocks : 16ll * num_sms)), 256, 0, s);
-  return p.q != nullptr ? launch_gamma<kBatch, true>(p, l) : launch_gamma<kBatch, false>(p, l);
+  const long long blocks = std::min((units + 7) / 8, 8ll * num_sms);
+  LaunchConfig l(dim3((unsigned)blocks), 256, 0, s);
+  if (p.gamma_k != nullptr)
+    return p.q != nullptr ? cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, true, true>, p)
+                          : cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, false, true>, p);
+  return p.q != nullptr ? cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, true, false>, p)
+                        : cudaLaunchKernelEx(&l.cfg, rope_head_kernel<kBatch, false, false>, p);
 }
 
 }  // namespace
@@ -180,7 +182,11 @@ cudaError_t launch_batch(RopeHeadParams& p, int num_sms, cudaStream_t s) {
 cudaError_t launch_rope_head(RopeHeadParams& p, int num_sms, cudaStream_t s) {
   const int per_tok = p.H * (p.d >> 3);
   p.group = per_tok >= 32 ? 32 : (per_tok >= 16 ? 16 : 8);
-  return launch_batch<2>(p, num_sms, s);
+  // A launch that leaves half of the warps idle is as long as one part takes: 320
+  // tokens of 12 x 128 with Q 3.2 us at two vectors a lane, 2.8 at one.  Past that
+  // two are faster (4680 tokens 17.3 us, 19.4 at one).
+  const long long rows = ((long long)p.n_nodes * p.T * per_tok + 31) / 32;
+  return rows <= 16ll * num_sms ? launch_batch<1>(p, num_sms, s) : launch_batch<2>(p, num_sms, s);
 }
 
 }  // namespace sva

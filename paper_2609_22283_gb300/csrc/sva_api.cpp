@@ -888,9 +888,7 @@ sva_status sva_rope_kv_write_headnorm(sva_cache* c, const sva_node* nodes, int32
   p.tab_w = reinterpret_cast<const float2*>(c->base + c->L.tab_w);
   p.gamma_k = gamma_k;
   p.gamma_q = has_q ? gamma_q : nullptr;
-  p.gamma = gamma_k == nullptr ? sva::HeadGamma::kNone
-            : gamma_heads == 1 ? sva::HeadGamma::kShared
-                               : sva::HeadGamma::kHeads;
+  p.gamma_heads = gamma_heads;
   p.eps = eps;
   p.T = c->L.T;
   p.H = g.num_heads;
