@@ -80,12 +80,18 @@ struct Ring {
 };
 
 // What goes with a Q tile, and the barriers of number i % 3 of the rings.
+template <bool kMask>
 struct alignas(16) Stage {
   float nl[kTile];      // -lse * log2(e) of its queries
-  uint64_t l_full;      // nl is there
-  uint64_t l_empty;     // both groups are done with it
+  uint32_t word[kMask ? 2 : 1][4][kMask ? kTile : 1];  // token masks: word w of key tile kt for each query
+  uint64_t l_full;      // nl, word and info are there
+  uint64_t l_empty;     // both groups are done with them
   uint64_t s_full[2], s_empty[2];  // S of each group
+  uint32_t info;        // masks: kItem bits, the query tile above them
 };
+// The item's key tiles that are marked; it has token words; frames hide keys of it.
+constexpr uint32_t kItemOn = 1, kItemWords = 4, kItemCausal = 8;
+constexpr int kItemTileShift = 8;
 
 struct Bars {
   uint64_t q_full[kMaxStages];   // a Q tile has landed
@@ -136,37 +142,49 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
       : "memory");
 }
 
+// One word to shared memory without a register, zero where `load` is false; and an
+// arrival on `bar` when this thread's copies so far have landed.
+__device__ __forceinline__ void cp_async_u32_if(uint32_t* dst, const uint32_t* src, bool load) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(load ? 4 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 // Caller data, by ordinary loads (see ptx.cuh).
 __device__ __forceinline__ float ld_f32_if(const float* p, bool load, float other) {
   return __uint_as_float(
       ld_global_u32_if(reinterpret_cast<const uint32_t*>(p), load, __float_as_uint(other)));
 }
 
-// The Q tiles of a unit in order: every (ref, query tile), or the marked ones of
-// a bitmap over ref * n_qt + tile.
+// The Q tiles of a unit in order: every (ref, query tile), or those marked for
+// either key tile in bitmaps over ref * n_qt + tile.
+constexpr int kMarkWords = SVA_MAX_NODES * kMaxQueryTiles / 32;
 template <bool kMask>
 struct Walk {
-  const uint32_t* marks;
-  int at, end, n_qt, r, qt;  // kMask: word of the bitmap, and the first item of ref r in `qt`
+  const uint32_t (*marks)[kMask ? kMarkWords : 1];
+  int at, end, n_qt, r, qt;  // kMask: word of the bitmaps, and the first item of ref r in `qt`
   uint32_t left;             // kMask: the word's bits still to come
-  __device__ __forceinline__ Walk(const uint32_t* marks_, int begin, int end_, int n_qt_)
+  __device__ __forceinline__ Walk(const uint32_t (*marks_)[kMask ? kMarkWords : 1], int begin, int end_, int n_qt_)
       : marks(marks_), at(begin), end(end_), n_qt(n_qt_), r(begin > 0 ? begin / n_qt_ : 0), qt(begin - r * n_qt_), left(0) {
     if constexpr (kMask) {
-      left = begin < end ? marks[begin >> 5] & (~0u << (begin & 31)) : 0u;
       at = begin >> 5;
+      left = begin < end ? word(at) & (~0u << (begin & 31)) : 0u;
       qt = r * n_qt;
     }
+  }
+  __device__ __forceinline__ uint32_t word(int w) const {
+    uint32_t m = marks[0][w] | marks[kMask ? 1 : 0][w];
+    if (w == end >> 5) m &= (1u << (end & 31)) - 1u;
+    return m;
   }
   // How many there are (before the first next).
   __device__ __forceinline__ int count() const {
     if constexpr (kMask) {
       int n = 0;
       const int words = (end + 31) >> 5;
-      for (int w = at; w < words; ++w) {
-        uint32_t m = w == at ? left : marks[w];
-        if (w == words - 1 && (end & 31)) m &= (1u << (end & 31)) - 1u;
-        n += __popc(m);
-      }
+      for (int w = at; w < words; ++w) n += __popc(w == at ? left : word(w));
       return n;
     } else {
       return end - at;
@@ -178,11 +196,10 @@ struct Walk {
       const int words = (end + 31) >> 5;
       while (left == 0u) {
         if (++at >= words) return false;
-        left = marks[at];
+        left = word(at);
       }
       const int i = (at << 5) + __ffs(left) - 1;
       left &= left - 1u;
-      if (i >= end) return false;
       while (i - qt >= n_qt) {
         qt += n_qt;
         ++r;
@@ -201,6 +218,11 @@ struct Walk {
       }
       return true;
     }
+  }
+  // Is the item marked for key tile kt?
+  __device__ __forceinline__ bool marked(int kt, int r_in, int qt_in) const {
+    const int i = r_in * n_qt + qt_in;
+    return (marks[kt][i >> 5] >> (i & 31)) & 1u;
   }
 };
 
@@ -231,8 +253,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   __shared__ Bars bars;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
-  __shared__ Stage stage[kRing];
-  __shared__ uint32_t marks[kMask ? SVA_MAX_NODES * kMaxQueryTiles / 32 : 1];
+  __shared__ Stage<kMask> stage[kRing];
+  __shared__ uint32_t marks[2][kMask ? kMarkWords : 1];
   __shared__ float part[kMaxWeightSplit][2 * kTile];  // rank 0: the cluster's partial sums
   __shared__ float half_sum[2][kTile];                // the second half's sums of a unit
   __shared__ volatile float part_lost;                // rank 0: a CTA of the cluster gave up
@@ -257,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       mbar_init(&bars.q_empty[s], 2);
     }
     for (int s = 0; s < kRing; ++s) {
-      mbar_init(&stage[s].l_full, 1);
+      mbar_init(&stage[s].l_full, kMask ? 33 : 1);  // nl, and with masks each lane's copies
       mbar_init(&stage[s].l_empty, 2 * kGroupWarps);
       for (int k = 0; k < 2; ++k) {
         mbar_init(&stage[s].s_full[k], 1);
@@ -280,38 +302,36 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   }
   pdl_wait();  // everything above is this CTA's own; what follows reads and writes global memory
   if constexpr (kMask) {
-    // Which Q tiles of this unit have anything visible, by the tile mask and the
-    // frames (token masks are looked at tile by tile, as they are staged).
+    // Which Q tiles have anything visible of either key tile of this unit, by the tile
+    // mask, the frames and the scan of the token masks.
     const Unit un = unit_of(p, u0);
     const int n_ref = p.first[un.si + 1] - p.first[un.si];
     const int n_all = n_ref * p.n_qt;
     for (int base = warp * 32; base < n_all; base += kThreads) {
       const int i = base + lane;
-      bool on = false;
+      bool on[2] = {false, false};
       if (i < n_all) {
         const int r = i / p.n_qt, qt = i - r * p.n_qt;
         const uint32_t ref = p.ref[p.first[un.si] + r];
         const int state = (ref >> kRefStateShift) & 31;
-        on = true;
-        if (p.tile_mask) {
-          const uint32_t* row =
-              p.tile_mask + ((size_t)(ref & 63) * p.n_qt + qt) * p.mask_words;
-          const int k = state * p.n_qt + 2 * un.kp;
-          on = ((row[k >> 5] >> (k & 31)) & 1u) != 0u;
-          if (2 * un.kp + 1 < p.n_qt) on = on || ((row[(k + 1) >> 5] >> ((k + 1) & 31)) & 1u) != 0u;
-        }
-        if (p.any_tile) {
-          const uint8_t* row = p.any_tile + ((size_t)(ref & 63) * p.n_qt + qt) * p.any_stride;
-          const int k = state * p.n_qt + 2 * un.kp;
-          on = on && (row[k] != 0 || (2 * un.kp + 1 < p.n_qt && row[k + 1] != 0));
-        }
-        if (state == 0 && (ref & kRefCausal)) {
-          const int last = min((qt + 1) * kTile, p.T) - 1;
-          on = on && last / p.frame_tokens >= 2 * un.kp * kTile / p.frame_tokens;
+        const size_t qrow = (size_t)(ref & 63) * p.n_qt + qt;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const int t = 2 * un.kp + kt, k = state * p.n_qt + t;
+          on[kt] = t < p.n_qt;
+          if (on[kt] && p.tile_mask) on[kt] = (p.tile_mask[qrow * p.mask_words + (k >> 5)] >> (k & 31)) & 1u;
+          if (on[kt] && p.any_tile) on[kt] = p.any_tile[qrow * p.any_stride + k] != 0;
+          if (on[kt] && state == 0 && (ref & kRefCausal)) {
+            const int last = min((qt + 1) * kTile, p.T) - 1;
+            on[kt] = last / p.frame_tokens >= t * kTile / p.frame_tokens;
+          }
         }
       }
-      const uint32_t m = __ballot_sync(0xffffffffu, on);
-      if (lane == 0) marks[base >> 5] = m;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const uint32_t m = __ballot_sync(0xffffffffu, on[kt]);
+        if (lane == 0) marks[kt][base >> 5] = m;
+      }
     }
   }
   tc_fence_before();
@@ -378,9 +398,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     Unit un = unit_of(p, u < p.units ? u : 0);
     Walk<kMask> walk = walk_of(un);
     float v[4];  // of queries k * 32 + lane
+    int r = 0, qt = 0;
     auto load = [&]() {  // the next item's; false past the last
       if (u >= p.units) return false;
-      int r, qt;
       while (!walk.next(r, qt)) {
         u += u_step;
         if (u >= p.units) return false;
@@ -396,21 +416,50 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       }
       return true;
     };
+    // Token words of an item: of each query (a lane's: k * 32 + lane) the four of either key tile.
+    auto copy_words = [&](Stage<kMask>& g) {
+      const uint32_t ref = p.ref[p.first[un.si] + r];
+      const int state = (int)(ref >> kRefStateShift) & 31;
+      const uint32_t* base = state == 0 ? p.own_mask : p.hist_mask;
+      const bool on[2] = {walk.marked(0, r, qt), walk.marked(1, r, qt)};
+      if (base != nullptr) {
+        const size_t query = state == 0 ? (size_t)p.own_words : (size_t)p.hist_states * p.hist_words;
+        const int w0 = un.kp * 8;  // first word of the pair of key tiles
+        const int words = (p.T + 31) / 32;
+        const uint32_t* row = base + ((size_t)(ref & 63u) * p.T + qt * kTile + lane) * query + w0 +
+                              (state == 0 ? 0 : (size_t)(state - 1) * p.hist_words);
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k, row += 32 * query) {
+          const bool in = qt * kTile + k * 32 + lane < p.T;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool load = in && on[j >> 2] && w0 + j < words;
+            cp_async_u32_if(&g.word[kMask ? j >> 2 : 0][j & 3][kMask ? k * 32 + lane : 0], load ? row + j : base, load);
+          }
+        }
+      }
+      if (lane == 0)
+        g.info = (on[0] ? kItemOn : 0u) | (on[1] ? kItemOn << 1 : 0u) | (base != nullptr ? kItemWords : 0u) |
+                 (state == 0 && (ref & kRefCausal) ? kItemCausal : 0u) | (uint32_t)qt << kItemTileShift;
+      cp_async_arrive(&g.l_full);
+    };
     bool ok = true;
     bool more = load();
     Ring it;
     while (more) {
-      Stage& g = stage[it.at];
+      Stage<kMask>& g = stage[it.at];
       ok = __all_sync(0xffffffffu, mbar_wait(&g.l_empty, it.phase ^ 1u, &abort_flag, tmo)) != 0;
       if (!ok) break;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         g.nl[k * 32 + lane] = v[k] == -INFINITY ? -INFINITY : v[k] * -1.4426950408889634f;
+      if constexpr (kMask) copy_words(g);
       __syncwarp();
       if (lane == 0) mbar_arrive(&g.l_full);
       it.step();
       more = load();
     }
+    if constexpr (kMask) asm volatile("cp.async.wait_all;" ::: "memory");  // no copy outlives the CTA
     if (!ok && lane == 0) record_timeout(p, &abort_flag);
   } else if (warp < 4) {
     // ------------------------------------------------------------ MMA issuers
@@ -511,44 +560,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         ok = copy_k();
         if (!ok) break;
       }
-      // Masks: this warp's 32 keys for query half * 64 + c * 32 + lane of the item,
-      // a bit a key, loaded an item ahead.
-      uint32_t seen[2] = {0u, 0u}, seen_next[2] = {0u, 0u};
-      auto load_seen = [&]() {
-        int r, qt;
-        if (!walk.next(r, qt)) return;
-        const uint32_t ref = p.ref[p.first[un.si] + r];
-        const int node = (int)(ref & 63u), state = (int)(ref >> kRefStateShift) & 31;
-        const int key0 = key - lane;
-        bool tile_on = true;
-        if (p.tile_mask) {
-          const uint32_t* row_m = p.tile_mask + ((size_t)node * p.n_qt + qt) * p.mask_words;
-          const int k = state * p.n_qt + 2 * un.kp + kt;
-          tile_on = has_keys && ((row_m[k >> 5] >> (k & 31)) & 1u) != 0u;
-        }
-        const uint32_t* base = state == 0 ? p.own_mask : p.hist_mask;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int q = qt * kTile + half * 64 + c * 32 + lane;
-          const size_t qrow = (size_t)node * p.T + q;
-          const uint32_t* w = state == 0 ? base + qrow * p.own_words
-                                         : base + (qrow * p.hist_states + (state - 1)) * p.hist_words;
-          const bool on = tile_on && has_keys && q < p.T;
-          seen_next[c] = ld_global_u32_if(w + (key0 >> 5), base != nullptr && on, on ? ~0u : 0u);
-          if (state == 0 && (ref & kRefCausal)) {  // keys up to the end of the query's frame
-            const int n = (q / p.frame_tokens + 1) * p.frame_tokens - key0;
-            if (n < 32) seen_next[c] &= n <= 0 ? 0u : (1u << n) - 1u;
-          }
-        }
-      };
-      if constexpr (kMask) load_seen();
+      const int first_query = key / p.frame_tokens * p.frame_tokens;  // that sees this key under frame causality
       while (left > 0) {
-        Stage& g = stage[it.at];
-        if constexpr (kMask) {
-          seen[0] = seen_next[0];
-          seen[1] = seen_next[1];
-          load_seen();
-        }
+        Stage<kMask>& g = stage[it.at];
         // both normally tested in one round trip
         const bool lok = mbar_try_wait(&g.l_full, it.phase);
         const bool sok = mbar_try_wait(&g.s_full[kt], it.phase);
@@ -603,34 +617,48 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           __syncwarp(); if (lane == 0) mbar_arrive(&g.s_empty[kt]);
           add(s1, 3, false, 0u);
         } else {
+          const uint32_t info = g.info;
+          const bool worded = info & kItemWords, causal = info & kItemCausal;
+          const int q0 = (int)(info >> kItemTileShift) * kTile + half * 64;  // this warp's first query
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            // a query that saw nothing adds nothing, whatever its row holds
-            uint32_t w = g.nl[half * 64 + c * 32 + lane] == -INFINITY ? 0u : seen[c];
-            // no sum is kept for the keys past the slot's end: as good as seen
-            const int past = p.T - (key - lane);
-            const uint32_t all = past < 32 && past > 0 ? w | (~0u << past) : w;
-            if (!__any_sync(0xffffffffu, w != 0u)) continue;
-            tmem_ld16(scol + c * 32, s0);
-            tmem_wait_ld16(s0);
-            tmem_ld16(scol + c * 32 + 16, s1);
-            if (__all_sync(0xffffffffu, all == ~0u)) {
-              add(s0, 2 * c, false, 0u);
-              tmem_wait_ld16(s1);
-              add(s1, 2 * c + 1, false, 0u);
-            } else {
-              // a bit a query for this lane's key: the 32 x 32 bits transposed
+          for (int c = 0; has_keys && (info & (kItemOn << kt)) && c < 2; ++c) {
+            // this warp's 32 keys for query c * 32 + lane; a query past T, or that saw
+            // nothing, adds nothing, whatever its row holds
+            const int q = half * 64 + c * 32 + lane;
+            uint32_t w = worded ? g.word[kMask ? kt : 0][q4][kMask ? q : 0] : ~0u;
+            if (g.nl[q] == -INFINITY) w = 0u;
+            uint32_t bits = __ballot_sync(0xffffffffu, w != 0u);  // a bit a query, for this lane's key
+            if (bits == 0u) continue;
+            if (worded && !__all_sync(0xffffffffu, w == ~0u)) {
+              bits = w;  // the 32 x 32 bits transposed
 #pragma unroll
               for (int j = 16; j > 0; j >>= 1) {
                 const uint32_t m = j == 16 ? 0x0000FFFFu : j == 8 ? 0x00FF00FFu : j == 4 ? 0x0F0F0F0Fu
                                                         : j == 2  ? 0x33333333u
                                                                   : 0x55555555u;
-                const uint32_t y = __shfl_xor_sync(0xffffffffu, w, j);
-                w = (lane & j) ? (w & ~m) | ((y >> j) & m) : (w & m) | ((y & m) << j);
+                const uint32_t y = __shfl_xor_sync(0xffffffffu, bits, j);
+                bits = (lane & j) ? (bits & ~m) | ((y >> j) & m) : (bits & m) | ((y & m) << j);
               }
-              add(s0, 2 * c, true, w);
+            }
+            if (causal) {
+              const int hidden = first_query - (q0 + c * 32);  // queries ahead of the key's frame
+              if (hidden > 0) bits = hidden < 32 ? bits & (~0u << hidden) : 0u;
+              if (!__any_sync(0xffffffffu, bits != 0u)) continue;
+            }
+            const uint32_t col = scol + (uint32_t)(c * 32);
+            tmem_ld16(col, s0);
+            tmem_wait_ld16(s0);
+            // no sum is kept for the keys past the slot's end
+            if (__all_sync(0xffffffffu, bits == ~0u || !mine)) {
+              tmem_ld16(col + 16, s1);
+              add(s0, 2 * c, false, 0u);
               tmem_wait_ld16(s1);
-              add(s1, 2 * c + 1, true, w >> 16);
+              add(s1, 2 * c + 1, false, 0u);
+            } else {
+              tmem_ld16(col + 16, s1);
+              add(s0, 2 * c, true, bits);
+              tmem_wait_ld16(s1);
+              add(s1, 2 * c + 1, true, bits >> 16);
             }
           }
           tc_fence_before();
