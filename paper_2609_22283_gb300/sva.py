@@ -154,20 +154,17 @@ def _tok_major(t: torch.Tensor, name: str, n: int, T: int, H: int, d: int):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, T, H, d)}")
 
 
-def _token_rows(t: torch.Tensor, name: str, n: int, T: int, H: int, d: int) -> sva_token_rows:
-    """A bf16 [n][T][H][d] tensor whose tokens lie at one stride, each dense: a tensor of its own, or the
-    q, k or v part of a packed one."""
-    if t.dtype != torch.bfloat16 or not t.is_cuda:
-        raise ValueError(f"{name} must be a bf16 CUDA tensor")
-    if t.shape != (n, T, H, d):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, T, H, d)}")
+def _token_stride(t: torch.Tensor, name: str) -> int:
+    """The token stride of a [n][T][H][d] tensor whose tokens, of all nodes, lie at one stride with dense
+    [H][d] rows: a tensor of its own, or the q, k or v part of a packed one."""
+    n, T, H, d = t.shape
     node, tok, head, one = t.stride()
     if T == 1:  # the stride of a dimension of one element says nothing: the nodes are the tokens
         tok = node if n > 1 else H * d
     if (one != 1 or (H > 1 and head != d) or (n > 1 and node != T * tok)
             or (tok < H * d and n * T > 1)):
         raise ValueError(f"{name} must hold dense [H][d] rows at one token stride (strides {t.stride()})")
-    return sva_token_rows(t.data_ptr(), max(tok, H * d))
+    return max(tok, H * d)
 
 
 # ---------------------------------------------------------------- selection (host)
@@ -323,13 +320,23 @@ class Cache:
         RoPE and the cache write.  k_new, v_new, q: bf16 [n][T][H][d], dense or parts of a packed
         tensor; q_out: dense, receives Q' (None: q itself, which then is dense)."""
         arr, count = _node_array(nodes)
-        rk = _token_rows(k_new, "k_new", count, self.T, self.H, self.d)
-        rv = _token_rows(v_new, "v_new", count, self.T, self.H, self.d)
-        rq = None
+        T, H, d = self.T, self.H, self.d
+        shape, rows = (count, T, H, d), []
+        for t, nm in ((k_new, "k_new"), (v_new, "v_new"), (q, "q")):
+            if t is None and nm == "q":
+                rows.append(None)
+                continue
+            if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != shape:
+                raise ValueError(f"{nm} must be a bf16 CUDA tensor {list(shape)}")
+            st = t.stride()
+            tok = st[1]
+            if st != (T * tok, tok, d, 1) or tok < H * d:
+                tok = _token_stride(t, nm)
+            rows.append(sva_token_rows(t.data_ptr(), tok))
+        rk, rv, rq = rows
         if q is not None:
-            rq = _token_rows(q, "q", count, self.T, self.H, self.d)
             q_out = q if q_out is None else q_out
-            _tok_major(q_out, "q_out", count, self.T, self.H, self.d)
+            _tok_major(q_out, "q_out", count, T, H, d)
         elif q_out is not None or gamma_q is not None:
             raise ValueError("q_out and gamma_q are for calls with q")
         heads = 1
@@ -338,11 +345,12 @@ class Cache:
                 continue
             if gm.dtype != torch.float32 or not gm.is_cuda or not gm.is_contiguous():
                 raise ValueError(f"{nm} must be a contiguous fp32 CUDA tensor")
-            if gm.shape not in ((self.d,), (self.H, self.d)):
-                raise ValueError(f"{nm} has shape {tuple(gm.shape)}, expected [{self.d}] or [{self.H}][{self.d}]")
-            heads = self.H if gm.dim() == 2 else 1
-        if gamma_k is not None and gamma_q is not None and gamma_k.shape != gamma_q.shape:
-            raise ValueError("gamma_k and gamma_q must have the same shape")
+            dims = gm.dim()
+            if (dims != 1 or gm.numel() != d) and (dims != 2 or gm.shape != (H, d)):
+                raise ValueError(f"{nm} has shape {tuple(gm.shape)}, expected [{d}] or [{H}][{d}]")
+            if nm == "gamma_q" and gamma_k is not None and gamma_k.dim() != dims:
+                raise ValueError("gamma_k and gamma_q must have the same shape")
+            heads = H if dims == 2 else 1
         _check(_lib.sva_rope_kv_write_headnorm(
             self.handle, arr, count, ctypes.byref(rk), ctypes.byref(rv),
             ctypes.byref(rq) if rq is not None else None, q_out.data_ptr() if rq is not None else None,

@@ -297,6 +297,32 @@ def test_queries_that_saw_nothing_add_nothing(sva_mod):
     c.close()
 
 
+def test_scanned_token_masks(sva_mod):
+    """A launch long enough for the scan of its token masks: the same bits with it and without (no workspace)."""
+    c = Case(sva_mod, 1, 39, 50, 12, 64, _chain(2, 3))      # 1950 tokens, 16 tiles
+    T, n = c.T, 2
+    u = torch.arange(T, device="cuda")
+    own = ((u[:, None] - u[None, :]).abs() < 200)[None].expand(n, T, T).clone()
+    hist = own[:, :, None].expand(n, T, 3, T).clone()
+    hist[:, 128:256] = False               # a query tile without history
+    hist[:, :, 1, :300] = False
+    own[:, 7::97] = False
+    hist[:, 7::97] = False                 # queries that see nothing
+    words = dict(own_mask=_pack(own), hist_mask=_pack(hist))
+    c.attend(own=words["own_mask"], hist=words["hist_mask"])
+    out = torch.zeros(c.shape, device="cuda")
+    c.cache.attend_weights(c.nodes, c.q, c.lse, out, **words)
+    c.cache.set_workspace(None)
+    plain = torch.zeros(c.shape, device="cuda")
+    c.cache.attend_weights(c.nodes, c.q, c.lse, plain, **words)
+    assert c.cache.poll() == sva_mod.OK
+    assert torch.equal(out, plain)
+    want, bound, seen = c.ref(own=own, hist=hist)
+    for s in seen:
+        assert torch.all((out[s].double() - want[s]).abs() <= bound[s])
+    c.close()
+
+
 def test_long_chunk_sums(sva_mod):
     """16384 queries into every key's sum, one head, both at a few keys checked in 64 bits."""
     c = Case(sva_mod, 1, 128, 128, 1, 64, _chain(1, 0), spare=0)
