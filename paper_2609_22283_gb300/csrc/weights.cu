@@ -5,21 +5,23 @@
 // the attention's.  With them known no running maximum is needed and no V: one
 // product and one exponential a (query, key) pair, and sums over queries.
 //
-// So the product is taken the other way round, S^T = K Q^T: a key is a TMEM
-// lane, its thread holds 32 or 64 of its scores at a time and adds their
-// exponentials up in registers.  No score, weight or sum crosses threads; a
-// unit's sum over all its queries stays in one register and nothing is added
-// atomically, so results do not depend on the order of CTAs.
+// So the product is taken the other way round, S^T = K Q^T: a key is a TMEM lane,
+// and the threads that hold its scores add their exponentials up in registers.  No
+// score crosses threads, a unit's sum over all its queries stays in two registers
+// of two threads, and nothing is added atomically: results do not depend on the
+// order of CTAs.
 //
 // One unit is (slot, head, pair of 128-key tiles).  K (the A operand) is copied
 // to TMEM once a unit, as packed bf16, so that the MMAs read only Q from shared
 // memory (with both operands there M = N = 128 needs all of its 128 B a cycle);
 // Q tiles of 128 queries stream past it, for every node that sees the slot.
-//   warp 0     TMA producer: a unit's K tiles, then its Q tiles (4 stages);
-//   warp 2     -lse * log2(e) of a Q tile's rows (-inf past the last row) into
-//              the stage; with masks also the tile's visibility words;
+//   warp 0     TMA producer: a unit's K tiles, then its Q tiles (4 or 8 stages,
+//              freed by the MMAs' commits);
+//   warp 2     -lse * log2(e) of a Q tile's rows (-inf past the last row); with
+//              masks also the tile's token words, by copies that need no register;
 //   warps 1, 3 MMA issuers of key tiles 0 and 1;
-//   warps 4-11 sums: warps 4-7 key tile 0, warps 8-11 key tile 1, a thread a key.
+//   warps 4-19 sums: warps 4-11 key tile 0, warps 12-19 key tile 1; a warp takes 32
+//              keys and half of the queries.
 // TMEM: K0, K1 (d / 2 columns each), then three S buffers of 128 columns that the
 // steps (Q tile i, key tile kt) take in turn, n = 2 i + kt in buffer n % 3: the
 // two groups work in opposite phase and each S is issued while the group before
@@ -29,11 +31,31 @@
 // unit's K waits in shared memory, and a group copies it to TMEM when the last S
 // of the unit is complete, ahead of the sums over that S.
 //
+// What bounds it: the sums.  256 keys x 128 queries are 1024 cycles of the tensor
+// core at d = 128 (512 at 64) and 1024 of the exponential unit, which shares its
+// issue queue with the TMEM and shared-memory loads: that loop alone, without
+// barriers or MMAs, takes 1240 cycles, the kernel 1550 at d = 128 (4680 queries over
+// 18720 keys, 12 heads: 177 us, 1520 TFLOP/s; four such nodes over 32760 keys 1206
+// us, 1562), 1500 at 64 (2 x 2160 queries over 10800 keys, 16 heads: 138 us).  Taken
+// on the way, each on the first of these cases: eight summing warps with 128 queries
+// each 220 us, sixteen 206; ring positions counted instead of divided 195; Q stages
+// freed by the MMAs 193; scores read 16 columns at a time (32 leave a thread too few
+// of its 96 registers to overlap exponentials) 186; no branch while scores are on
+// their way from TMEM (the compiler waits for them at it) 177.  Not kept: eight
+// warps in that form 184; the next item's first scores loaded ahead 196 to 230; S in
+// halves of 64 queries with six buffers 209; both operands in shared memory 194; 2^x
+// by a polynomial for part of the scores (no gain in the loop alone).
+//
 // Launches with fewer units than SMs split a unit's Q tiles over a cluster; the
 // partial sums go to the first CTA's shared memory and are added in rank order.
-// Launches with masks (or frame causality) take one unit a CTA: a bitmap of the
-// (node, Q tile) pairs that have any visible tile is built first, and only those
-// are loaded and multiplied.
+// Launches with masks (or frame causality) take one unit a CTA: a bitmap for each
+// key tile of the (node, Q tile) pairs that have any visible pair, as far as the tile
+// mask, the frames and the scan of the token masks say, is built first, and only
+// tiles marked for either are loaded and multiplied.  A warp without a visible pair
+// in its 32 keys x 32 queries skips them; where all are visible it does as without
+// masks (tile masks with all bits set: 271 us on the first case above); else it hides
+// scores by the transposed bits (4680 queries over own and three history chunks, keys
+// within 6 patch rows and columns: 225 us, of which the scan takes 9).
 // All waits are bounded as in the attention kernel; a unit whose CTA gave up one
 // is not written.
 #include <mutex>
@@ -52,7 +74,7 @@ using namespace ptx;
 constexpr int kThreads = 640;
 constexpr int kRing = 3;  // S buffers and stages of log-sum-exps: item i uses number i % 3
 constexpr int kMaxStages = 8;
-constexpr int kGroupWarps = 8;
+constexpr int kGroupWarps = 8;  // of a key tile: four TMEM lane quarters x two halves of the queries
 
 template <int D>
 struct Cfg {
@@ -122,17 +144,22 @@ __device__ __forceinline__ void mma_ts_kmajor_x4(uint32_t d_tmem, uint32_t a_tme
       : "memory");
 }
 
+// Each thread reads 16 columns of its lane; not valid until tmem_wait_ld16(r) has run.
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(taddr));
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait_ld16(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
                :
                : "memory");
 }
+
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar, int32_t c0,
                                             int32_t c1) {
   asm volatile(
@@ -550,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       const int key = (un.kp * 2 + kt) * kTile + row;
       const size_t at = ((size_t)p.slot[un.si] * p.H + un.h) * p.T + key;
       const bool mine = key < p.T;
-      const bool has_keys = key - lane < p.T;  // this warp's part of the tile; K is not loaded past the slot
+      const bool has_keys = key - lane < p.T;  // the warp's part of the tile (K is not loaded past the slot)
       const float before = ld_f32_if(p.prev + at, p.prev != nullptr && mine && ns == 1, 0.0f);
       float total = 0.0f;
       const bool next_k = u + u_step < p.units;  // another unit's K is to follow
@@ -600,21 +627,21 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         uint32_t s0[16], s1[16];
         const uint32_t scol = tbase + lane_off + C::kColS + (uint32_t)(buf * kTile + half * 64);
         if constexpr (!kMask) {
-          {
-            tmem_ld16(scol, s0);
-            tmem_wait_ld16(s0);
-            tmem_ld16(scol + 16, s1);
-            add(s0, 0, false, 0u);
-            tmem_wait_ld16(s1);
-            tmem_ld16(scol + 32, s0);
-            add(s1, 1, false, 0u);
-            tmem_wait_ld16(s0);
-            tmem_ld16(scol + 48, s1);
-            add(s0, 2, false, 0u);
-            tmem_wait_ld16(s1);
-          }
+          // a warp without keys adds what it finds: a test here costs all others 3 to 8%
+          tmem_ld16(scol, s0);
+          tmem_wait_ld16(s0);
+          tmem_ld16(scol + 16, s1);
+          add(s0, 0, false, 0u);
+          tmem_wait_ld16(s1);
+          tmem_ld16(scol + 32, s0);
+          add(s1, 1, false, 0u);
+          tmem_wait_ld16(s0);
+          tmem_ld16(scol + 48, s1);
+          add(s0, 2, false, 0u);
+          tmem_wait_ld16(s1);
           tc_fence_before();
-          __syncwarp(); if (lane == 0) mbar_arrive(&g.s_empty[kt]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&g.s_empty[kt]);
           add(s1, 3, false, 0u);
         } else {
           const uint32_t info = g.info;
@@ -662,13 +689,15 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
             }
           }
           tc_fence_before();
-          __syncwarp(); if (lane == 0) mbar_arrive(&g.s_empty[kt]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&g.s_empty[kt]);
         }
         const uint64_t a = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
         float lo, hi;
         u2f(a, lo, hi);
         total += lo + hi;
-        __syncwarp(); if (lane == 0) mbar_arrive(&g.l_empty);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&g.l_empty);
         buf = buf == 0 ? 2 : buf - 1;  // two steps on, modulo 3
         it.step();
       }
@@ -719,6 +748,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   }
 
   // ---------------------------------------------------------------- teardown
+  // The commits that free the last Q stages have arrived before the CTA leaves.
+  if (warp == 0 && lane == 0)
+    for (int i = (q_issued > C::kStages ? q_issued - C::kStages : 0); !abort_flag && i < q_issued; ++i)
+      mbar_wait(&bars.q_empty[i % C::kStages], (uint32_t)(i / C::kStages) & 1u, &abort_flag, tmo);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
