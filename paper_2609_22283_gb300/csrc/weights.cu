@@ -51,11 +51,12 @@
 // Launches with masks (or frame causality) take one unit a CTA: a bitmap for each
 // key tile of the (node, Q tile) pairs that have any visible pair, as far as the tile
 // mask, the frames and the scan of the token masks say, is built first, and only
-// tiles marked for either are loaded and multiplied.  A warp without a visible pair
-// in its 32 keys x 32 queries skips them; where all are visible it does as without
-// masks (tile masks with all bits set: 271 us on the first case above); else it hides
-// scores by the transposed bits (4680 queries over own and three history chunks, keys
-// within 6 patch rows and columns: 225 us, of which the scan takes 9).
+// tiles marked for either are loaded and multiplied.  Items that no token mask and no
+// frame cuts are summed as without masks (tile masks with all bits set: 212 us on the
+// first case above); elsewhere a warp without a visible pair in its 32 keys x 32
+// queries skips them, and hides scores by the transposed bits where some are visible
+// (4680 queries over own and three history chunks, keys within 6 patch rows and
+// columns: 225 us, of which the scan takes 9; random bits 375).
 // All waits are bounded as in the attention kernel; a unit whose CTA gave up one
 // is not written.
 #include <mutex>
@@ -101,18 +102,25 @@ struct Ring {
   }
 };
 
+// The kernel's instances: without masks; tile masks and frame causality, where most
+// marked tiles are wholly visible; token masks (with any of them).
+enum class Masks { kNone, kTiles, kWords };
+
 // What goes with a Q tile, and the barriers of number i % 3 of the rings.
-template <bool kMask>
+template <bool kWords>
 struct alignas(16) Stage {
   float nl[kTile];      // -lse * log2(e) of its queries
-  uint32_t word[kMask ? 2 : 1][4][kMask ? kTile : 1];  // token masks: word w of key tile kt for each query
+  // token masks: word w of key tile kt for each query (rows of 132: eight words of
+  // four queries lie on 32 banks)
+  uint32_t word[kWords ? 8 : 1][kWords ? kTile + 4 : 4];
   uint64_t l_full;      // nl, word and info are there
   uint64_t l_empty;     // both groups are done with them
   uint64_t s_full[2], s_empty[2];  // S of each group
   uint32_t info;        // masks: kItem bits, the query tile above them
 };
-// The item's key tiles that are marked; it has token words; frames hide keys of it.
-constexpr uint32_t kItemOn = 1, kItemWords = 4, kItemCausal = 8;
+// The item's key tiles that are marked; it has token words; frames hide keys of it;
+// every pair of the marked tiles is visible.
+constexpr uint32_t kItemOn = 1, kItemWords = 4, kItemCausal = 8, kItemPlain = 16;
 constexpr int kItemTileShift = 8;
 
 struct Bars {
@@ -174,6 +182,9 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
 __device__ __forceinline__ void cp_async_u32_if(uint32_t* dst, const uint32_t* src, bool load) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(load ? 4 : 0)
                : "memory");
+}
+__device__ __forceinline__ void cp_async_u32(uint32_t* dst, const uint32_t* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -271,16 +282,17 @@ __device__ __forceinline__ void record_timeout(const WeightParams& p, volatile i
   atomicCAS(p.status, kStatusOk, kStatusTimeout);
 }
 
-template <int D, bool kMask>
+template <int D, Masks kMasks>
 __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_constant__ WeightParams p) {
   using C = Cfg<D>;
+  constexpr bool kMask = kMasks != Masks::kNone, kWords = kMasks == Masks::kWords;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   __shared__ Bars bars;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
-  __shared__ Stage<kMask> stage[kRing];
+  __shared__ Stage<kWords> stage[kRing];
   __shared__ uint32_t marks[2][kMask ? kMarkWords : 1];
   __shared__ float part[kMaxWeightSplit][2 * kTile];  // rank 0: the cluster's partial sums
   __shared__ float half_sum[2][kTile];                // the second half's sums of a unit
@@ -306,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       mbar_init(&bars.q_empty[s], 2);
     }
     for (int s = 0; s < kRing; ++s) {
-      mbar_init(&stage[s].l_full, kMask ? 33 : 1);  // nl, and with masks each lane's copies
+      mbar_init(&stage[s].l_full, kWords ? 33 : 1);  // nl, and with masks each lane's copies
       mbar_init(&stage[s].l_empty, 2 * kGroupWarps);
       for (int k = 0; k < 2; ++k) {
         mbar_init(&stage[s].s_full[k], 1);
@@ -443,50 +455,62 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       }
       return true;
     };
-    // Token words of an item: of each query (a lane's: k * 32 + lane) the four of either key tile.
-    auto copy_words = [&](Stage<kMask>& g) {
+    // What the masks say of an item, and its token words: of each query (a lane's: k * 32 +
+    // lane) the four of either key tile.
+    auto describe = [&](Stage<kWords>& g) {
       const uint32_t ref = p.ref[p.first[un.si] + r];
       const int state = (int)(ref >> kRefStateShift) & 31;
       const uint32_t* base = state == 0 ? p.own_mask : p.hist_mask;
       const bool on[2] = {walk.marked(0, r, qt), walk.marked(1, r, qt)};
-      if (base != nullptr) {
+      if (kWords && base != nullptr) {
         const size_t query = state == 0 ? (size_t)p.own_words : (size_t)p.hist_states * p.hist_words;
         const int w0 = un.kp * 8;  // first word of the pair of key tiles
         const int words = (p.T + 31) / 32;
-        const uint32_t* row = base + ((size_t)(ref & 63u) * p.T + qt * kTile + lane) * query + w0 +
+        // eight lanes take the eight words of a query, four queries at a time
+        const int j = lane & 7, q = lane >> 3;
+        const uint32_t* row = base + ((size_t)(ref & 63u) * p.T + qt * kTile + q) * query + w0 + j +
                               (state == 0 ? 0 : (size_t)(state - 1) * p.hist_words);
-#pragma unroll 1
-        for (int k = 0; k < 4; ++k, row += 32 * query) {
-          const bool in = qt * kTile + k * 32 + lane < p.T;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const bool load = in && on[j >> 2] && w0 + j < words;
-            cp_async_u32_if(&g.word[kMask ? j >> 2 : 0][j & 3][kMask ? k * 32 + lane : 0], load ? row + j : base, load);
+        const size_t step = 4 * query;
+        uint32_t* dst = &g.word[kWords ? j : 0][q];
+        if (on[0] && on[1] && w0 + 8 <= words && (qt + 1) * kTile <= p.T) {  // nothing to leave out
+#pragma unroll 16
+          for (int k = 0; k < kTile / 4; ++k, row += step) cp_async_u32(dst + 4 * k, row);
+        } else {
+          const bool load = on[j >> 2] && w0 + j < words;
+          const int rows = load ? p.T - qt * kTile : 0;
+#pragma unroll 8
+          for (int k = 0; k < kTile / 4; ++k, row += step) {
+            const bool in = q + 4 * k < rows;
+            cp_async_u32_if(dst + 4 * k, in ? row : base, in);
           }
         }
       }
+      const bool causal = state == 0 && (ref & kRefCausal);
+      // rows past T hold +inf, queries that saw nothing -inf
+      const bool plain = !kWords && !causal &&
+                         __all_sync(0xffffffffu, isfinite(v[0]) && isfinite(v[1]) && isfinite(v[2]) && isfinite(v[3]));
       if (lane == 0)
-        g.info = (on[0] ? kItemOn : 0u) | (on[1] ? kItemOn << 1 : 0u) | (base != nullptr ? kItemWords : 0u) |
-                 (state == 0 && (ref & kRefCausal) ? kItemCausal : 0u) | (uint32_t)qt << kItemTileShift;
-      cp_async_arrive(&g.l_full);
+        g.info = (plain ? kItemPlain : 0u) | (on[0] ? kItemOn : 0u) | (on[1] ? kItemOn << 1 : 0u) | (base != nullptr ? kItemWords : 0u) |
+                 (causal ? kItemCausal : 0u) | (uint32_t)qt << kItemTileShift;
+      if constexpr (kWords) cp_async_arrive(&g.l_full);
     };
     bool ok = true;
     bool more = load();
     Ring it;
     while (more) {
-      Stage<kMask>& g = stage[it.at];
+      Stage<kWords>& g = stage[it.at];
       ok = __all_sync(0xffffffffu, mbar_wait(&g.l_empty, it.phase ^ 1u, &abort_flag, tmo)) != 0;
       if (!ok) break;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         g.nl[k * 32 + lane] = v[k] == -INFINITY ? -INFINITY : v[k] * -1.4426950408889634f;
-      if constexpr (kMask) copy_words(g);
+      if constexpr (kMask) describe(g);
       __syncwarp();
       if (lane == 0) mbar_arrive(&g.l_full);
       it.step();
       more = load();
     }
-    if constexpr (kMask) asm volatile("cp.async.wait_all;" ::: "memory");  // no copy outlives the CTA
+    if constexpr (kWords) asm volatile("cp.async.wait_all;" ::: "memory");  // no copy outlives the CTA
     if (!ok && lane == 0) record_timeout(p, &abort_flag);
   } else if (warp < 4) {
     // ------------------------------------------------------------ MMA issuers
@@ -589,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       }
       const int first_query = key / p.frame_tokens * p.frame_tokens;  // that sees this key under frame causality
       while (left > 0) {
-        Stage<kMask>& g = stage[it.at];
+        Stage<kWords>& g = stage[it.at];
         // both normally tested in one round trip
         const bool lok = mbar_try_wait(&g.l_full, it.phase);
         const bool sok = mbar_try_wait(&g.s_full[kt], it.phase);
@@ -626,7 +650,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         };
         uint32_t s0[16], s1[16];
         const uint32_t scol = tbase + lane_off + C::kColS + (uint32_t)(buf * kTile + half * 64);
-        if constexpr (!kMask) {
+        const uint32_t info = kMask ? g.info : 0u;
+        // (with token words that test costs the others 3 to 7%)
+        const uint32_t plain = kItemPlain | kItemOn << kt;
+        if (!kMask || (!kWords && (info & plain) == plain)) {
           // a warp without keys adds what it finds: a test here costs all others 3 to 8%
           tmem_ld16(scol, s0);
           tmem_wait_ld16(s0);
@@ -644,15 +671,14 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           if (lane == 0) mbar_arrive(&g.s_empty[kt]);
           add(s1, 3, false, 0u);
         } else {
-          const uint32_t info = g.info;
-          const bool worded = info & kItemWords, causal = info & kItemCausal;
+          const bool worded = kWords && (info & kItemWords), causal = info & kItemCausal;
           const int q0 = (int)(info >> kItemTileShift) * kTile + half * 64;  // this warp's first query
 #pragma unroll
           for (int c = 0; has_keys && (info & (kItemOn << kt)) && c < 2; ++c) {
             // this warp's 32 keys for query c * 32 + lane; a query past T, or that saw
             // nothing, adds nothing, whatever its row holds
             const int q = half * 64 + c * 32 + lane;
-            uint32_t w = worded ? g.word[kMask ? kt : 0][q4][kMask ? q : 0] : ~0u;
+            uint32_t w = worded ? g.word[kWords ? kt * 4 + q4 : 0][kWords ? q : 0] : ~0u;
             if (g.nl[q] == -INFINITY) w = 0u;
             uint32_t bits = __ballot_sync(0xffffffffu, w != 0u);  // a bit a query, for this lane's key
             if (bits == 0u) continue;
@@ -777,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   }
 }
 
-template <int D, bool kMask>
+template <int D, Masks kMasks>
 cudaError_t launch(const WeightParams& p, int grid, cudaStream_t s) {
   static std::mutex mu;
   static bool configured[64] = {};
@@ -788,21 +814,28 @@ cudaError_t launch(const WeightParams& p, int grid, cudaStream_t s) {
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!configured[dev]) {
-      e = cudaFuncSetAttribute(weights_kernel<D, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      e = cudaFuncSetAttribute(weights_kernel<D, kMasks>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                Cfg<D>::kSmemBytes);
       if (e != cudaSuccess) return e;
       configured[dev] = true;
     }
   }
   LaunchConfig l(dim3((unsigned)grid), kThreads, Cfg<D>::kSmemBytes, s, p.n_split > 1 ? p.n_split : 0);
-  return cudaLaunchKernelEx(&l.cfg, weights_kernel<D, kMask>, p);
+  return cudaLaunchKernelEx(&l.cfg, weights_kernel<D, kMasks>, p);
 }
 
 }  // namespace
 
 cudaError_t launch_weights(const WeightParams& p, int head_dim, int grid, cudaStream_t s) {
-  if (head_dim == 128) return p.masked ? launch<128, true>(p, grid, s) : launch<128, false>(p, grid, s);
-  if (head_dim == 64) return p.masked ? launch<64, true>(p, grid, s) : launch<64, false>(p, grid, s);
+  const bool words = p.own_mask != nullptr || p.hist_mask != nullptr;
+  if (head_dim == 128)
+    return words      ? launch<128, Masks::kWords>(p, grid, s)
+           : p.masked ? launch<128, Masks::kTiles>(p, grid, s)
+                      : launch<128, Masks::kNone>(p, grid, s);
+  if (head_dim == 64)
+    return words      ? launch<64, Masks::kWords>(p, grid, s)
+           : p.masked ? launch<64, Masks::kTiles>(p, grid, s)
+                      : launch<64, Masks::kNone>(p, grid, s);
   return cudaErrorInvalidValue;
 }
 
