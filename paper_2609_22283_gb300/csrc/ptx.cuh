@@ -68,42 +68,6 @@ __device__ __forceinline__ uint32_t ld_global_u32_if(const uint32_t* p, bool loa
   return v;
 }
 
-// ---------------------------------------------------------------- arithmetic
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Pairs of fp32 in a 64-bit register, two lanes an instruction.
-__device__ __forceinline__ uint64_t f2u(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-
-__device__ __forceinline__ void u2f(uint64_t r, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r));
-}
-
-// (a0, a1) * bb + cc, two lanes in one instruction
-__device__ __forceinline__ void ffma2(float& o0, float& o1, float a0, float a1, uint64_t bb,
-                                      uint64_t cc) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(f2u(a0, a1)), "l"(bb), "l"(cc));
-  u2f(r, o0, o1);
-}
-
-__device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fadd2(uint64_t a, float b0, float b1) {
-  return fadd2(a, f2u(b0, b1));
-}
-
 // ---------------------------------------------------------------- mbarrier
 
 __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {

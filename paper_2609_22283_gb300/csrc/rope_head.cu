@@ -12,8 +12,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include "internal.h"
 #include "ptx.cuh"
+#include "rope_head.h"
 
 namespace sva {
 namespace {

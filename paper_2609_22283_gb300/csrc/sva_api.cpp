@@ -23,6 +23,7 @@
 #include "condense.h"
 #include "internal.h"
 #include "proj.h"
+#include "rope_head.h"
 #include "sva.h"
 #include "weights.h"
 

@@ -132,6 +132,33 @@ struct Bars {
   uint64_t drain;
 };
 
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Pairs of fp32 in a 64-bit register, two lanes an instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t r, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r));
+}
+// (a0, a1) * b + c
+__device__ __forceinline__ void fma2(float& o0, float& o1, float a0, float a1, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a0, a1)), "l"(b), "l"(c));
+  unpair(r, o0, o1);
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Four MMAs over 64 elements of K, A from TMEM, B K-major in shared memory;
 // the first accumulates where `accumulate` says.
 __device__ __forceinline__ void mma_ts_kmajor_x4(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
@@ -566,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     const int q4 = warp & 3;  // TMEM lane quarter this warp may access
     const int row = q4 * 32 + lane;
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
-    const uint64_t sl2x2 = f2u(p.scale_log2, p.scale_log2);
+    const uint64_t sl2x2 = pair(p.scale_log2, p.scale_log2);
     bool ok = true;
     int n_unit = 0, done = 0, buf = kt;
     Ring it;
@@ -636,16 +663,16 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           for (int e = 0; e < 16; e += 4) {
             const ulonglong2 n = nl2[e >> 2];
             float x0, x1, x2, x3;
-            ffma2(x0, x1, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), sl2x2, n.x);
-            ffma2(x2, x3, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]), sl2x2, n.y);
+            fma2(x0, x1, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), sl2x2, n.x);
+            fma2(x2, x3, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]), sl2x2, n.y);
             if (some) {
               if (!((bits >> e) & 1u)) x0 = -INFINITY;
               if (!((bits >> (e + 1)) & 1u)) x1 = -INFINITY;
               if (!((bits >> (e + 2)) & 1u)) x2 = -INFINITY;
               if (!((bits >> (e + 3)) & 1u)) x3 = -INFINITY;
             }
-            acc[(e >> 1) & 3] = fadd2(acc[(e >> 1) & 3], ex2(x0), ex2(x1));
-            acc[((e >> 1) + 1) & 3] = fadd2(acc[((e >> 1) + 1) & 3], ex2(x2), ex2(x3));
+            acc[(e >> 1) & 3] = add2(acc[(e >> 1) & 3], pair(ex2(x0), ex2(x1)));
+            acc[((e >> 1) + 1) & 3] = add2(acc[((e >> 1) + 1) & 3], pair(ex2(x2), ex2(x3)));
           }
         };
         uint32_t s0[16], s1[16];
@@ -718,9 +745,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           __syncwarp();
           if (lane == 0) mbar_arrive(&g.s_empty[kt]);
         }
-        const uint64_t a = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+        const uint64_t a = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
         float lo, hi;
-        u2f(a, lo, hi);
+        unpair(a, lo, hi);
         total += lo + hi;
         __syncwarp();
         if (lane == 0) mbar_arrive(&g.l_empty);
