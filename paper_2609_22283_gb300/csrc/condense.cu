@@ -13,8 +13,14 @@
 // equal (tokens that nothing attended); or the other digits are found like the
 // first, each CTA reading all histograms.  Then what stays is ranked: everything
 // above the key, and of the candidates equal to it the first ones.  Counts and ranks
-// are integers, so the result does not depend on the order of the atomics.
-// condense_gather_kernel then copies the kept rows of K and V: bound by HBM.
+// are integers, so the result does not depend on the order of the atomics.  What
+// bounds it is the chain of these steps: 28080 candidates in eight CTAs take 10.5 us,
+// of which the loads 2.0, three cluster barriers 2.4, what passes between the CTAs
+// 2.5, four scans of a block 2.0.  With each digit's eight histograms read by every
+// CTA it was 15.6 us.
+// condense_gather_kernel then copies the kept rows of K and V: bound by HBM (4680 rows
+// of 12 heads of 128, 57 MB, 10.2 us; of 40 heads, 192 MB, 26.9 us: 5.6 and 7.1 TB/s
+// with part of the rows in L2).
 #include <algorithm>
 #include <mutex>
 
@@ -72,26 +78,27 @@ __device__ __forceinline__ void cluster_wait() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Exclusive sum over the block, in thread order; `all`: the sum of all.  Two
-// counts of up to 2^31 in one 64-bit sum.  Every thread calls it.
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* warp_sum, uint64_t* all) {
+// Exclusive sum over the block, in thread order; `all`: the sum of all.  Every
+// thread calls it.
+template <typename Sum>
+__device__ __forceinline__ Sum block_scan(Sum v, Sum* warp_sum, Sum* all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t s = v;
+  Sum s = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint64_t a = __shfl_up_sync(0xffffffffu, s, o);
+    const Sum a = __shfl_up_sync(0xffffffffu, s, o);
     if (lane >= o) s += a;
   }
   if (lane == 31) warp_sum[warp] = s;
   __syncthreads();
-  uint64_t w = lane < kSelWarps ? warp_sum[lane] : 0;  // every warp sums all of them
+  Sum w = lane < kSelWarps ? warp_sum[lane] : 0;  // every warp sums all of them
 #pragma unroll
   for (int o = 1; o < kSelWarps; o <<= 1) {
-    const uint64_t a = __shfl_up_sync(0xffffffffu, w, o);
+    const Sum a = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += a;
   }
   *all = __shfl_sync(0xffffffffu, w, kSelWarps - 1);
-  const uint64_t before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+  const Sum before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
   return s - v + (warp > 0 ? before : 0);
 }
 
@@ -100,10 +107,10 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* warp_sum, u
 struct Digit {
   uint32_t digit, above, here;  // candidates above the digit, and with it
 };
-__device__ __forceinline__ Digit find_digit(uint4 bins, int need, uint64_t* warp_sum, Digit* found) {
-  uint64_t all;
+__device__ __forceinline__ Digit find_digit(uint4 bins, int need, uint32_t* warp_sum, Digit* found) {
+  uint32_t all;
   const uint32_t total = bins.x + bins.y + bins.z + bins.w;
-  uint32_t at = (uint32_t)block_scan(total, warp_sum, &all);
+  uint32_t at = block_scan(total, warp_sum, &all);
   const uint32_t line = (uint32_t)need;
   if (at < line && at + total >= line) {
     uint32_t digit = (uint32_t)(kBins - 1 - 4 * threadIdx.x), here = bins.w;
@@ -135,7 +142,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
   __shared__ alignas(16) uint32_t hist[2][kBins];  // of this CTA's candidates
   __shared__ alignas(16) uint32_t sums[kBins];     // the first digit's, of the cluster
   __shared__ uint32_t list[kListKeys];             // the cluster's candidates with the first digit
-  __shared__ uint64_t warp_sum[6][kSelWarps];      // of each scan
+  __shared__ uint32_t warp_sum[5][kSelWarps];      // of each digit
+  __shared__ uint64_t warp_count[kSelWarps];
   __shared__ Digit found[5];
   __shared__ alignas(16) uint32_t match_sh[4];     // this CTA's candidates with the first digit: how many, least, largest
   __shared__ alignas(16) uint32_t count_sh[4];     // this CTA's candidates above the line and on it
@@ -162,15 +170,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
   if constexpr (kCluster > 1) cluster_arrive();    // the sums are clear
   ptx::pdl_wait();
   const uint32_t* weight = reinterpret_cast<const uint32_t*>(p.weight);
+  const uint32_t inv_t = 0xFFFFFFFFu / (uint32_t)p.T;
   auto load = [&](int e) {  // candidate e of the head
-    const int i = e / p.T;
+    int i = (int)__umulhi((uint32_t)e, inv_t);  // e / T or one less: e < 2^20
+    if ((i + 1) * p.T <= e) ++i;
     return weight[((size_t)p.slot[i] * p.H + h) * p.T + (e - i * p.T)];
   };
   auto bits_at = [&](int j) { return hold ? held[j] : load(e0 + j); };
   __syncthreads();
 
   // First digit: the few bins in use are added to every CTA's sums.
-#pragma unroll 4
+#pragma unroll 8
   for (int j = tid; j < count; j += kSelThreads) {
     const uint32_t w = load(e0 + j);
     if (hold) held[j] = w;
@@ -199,12 +209,32 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
 
   // The candidates that match: their keys where they are few, their range.
   uint32_t least = ~0u, most = 0;
-  for (int j = tid; j < count; j += kSelThreads) {
-    const uint32_t k = key_of(bits_at(j));
-    if (((k ^ prefix) >> 21) != 0u) continue;
-    least = min(least, k);
-    most = max(most, k);
-    if (listed) mine[atomicAdd(&match_sh[0], 1u)] = k;
+  constexpr int kBlock = 8;  // candidates a thread in one step: one count a warp and step
+  for (int base = 0; base < count; base += kBlock * kSelThreads) {
+    uint32_t key[kBlock], bits = 0;
+#pragma unroll
+    for (int u = 0; u < kBlock; ++u) {
+      const int j = base + u * kSelThreads + tid;
+      key[u] = j < count ? key_of(bits_at(j)) : ~prefix;
+      if (((key[u] ^ prefix) >> 21) == 0u) {
+        bits |= 1u << u;
+        least = min(least, key[u]);
+        most = max(most, key[u]);
+      }
+    }
+    if (!listed || !__any_sync(0xffffffffu, bits != 0u)) continue;
+    uint32_t at = (uint32_t)__popc(bits);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, at, o);
+      if (lane >= o) at += x;
+    }
+    uint32_t first_at = 0;
+    if (lane == 31) first_at = atomicAdd(&match_sh[0], at);
+    at += __shfl_sync(0xffffffffu, first_at, 31) - (uint32_t)__popc(bits);
+#pragma unroll
+    for (int u = 0; u < kBlock; ++u)
+      if (bits >> u & 1u) mine[at++] = key[u];
   }
   least = __reduce_min_sync(0xffffffffu, least);
   most = __reduce_max_sync(0xffffffffu, most);
@@ -237,12 +267,16 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
     // Every CTA gathers the cluster's and finds the other digits for itself.
     const uint32_t* keys = mine;
     if constexpr (kCluster > 1) {
-      uint32_t at = 0;
+#pragma unroll 4
+      for (uint32_t j = tid; j < d.here; j += kSelThreads) {
+        uint32_t c = 0, at = j;  // its CTA, its place there
 #pragma unroll
-      for (int c = 0; c < kCluster; ++c) {
-        for (uint32_t j = tid; j < match[c].x; j += kSelThreads)
-          list[at + j] = ld_cluster_u32(ptx::mapa_shared(ptx::smem_u32(mine + j), (uint32_t)c));
-        at += match[c].x;
+        for (int k = 0; k < kCluster - 1; ++k)
+          if (c == (uint32_t)k && at >= match[k].x) {
+            at -= match[k].x;
+            ++c;
+          }
+        list[j] = ld_cluster_u32(ptx::mapa_shared(ptx::smem_u32(mine + at), c));
       }
       keys = list;
       __syncthreads();
@@ -311,7 +345,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
     equal += k == prefix;
   }
   uint64_t all;
-  const uint64_t at = block_scan((uint64_t)above << 32 | equal, warp_sum[5], &all);
+  const uint64_t at = block_scan((uint64_t)above << 32 | equal, warp_count, &all);
   int kept = 0, level = 0;  // kept and equal candidates of the CTAs before this one
   if constexpr (kCluster > 1) {
     if (tid == 0) {

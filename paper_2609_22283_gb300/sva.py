@@ -259,6 +259,9 @@ class Cache:
         self.T = g.frames * g.grid_h * g.grid_w
         self.Tpad = (self.T + 127) // 128 * 128
         self._w_shape = (int(g.num_slots), self.H, self.T)
+        # arguments of rope_kv_write_headnorm, made once (a cache has one host thread at a time)
+        self._rows = [sva_token_rows() for _ in range(3)]
+        self._rows_at = [ctypes.byref(r) for r in self._rows]
         handle = ctypes.c_void_p()
         with torch.cuda.device(buf.device):
             _check(lib.sva_cache_create(ctypes.byref(g), buf.data_ptr(),
@@ -321,19 +324,15 @@ class Cache:
         tensor; q_out: dense, receives Q' (None: q itself, which then is dense)."""
         arr, count = _node_array(nodes)
         T, H, d = self.T, self.H, self.d
-        shape, rows = (count, T, H, d), []
-        for t, nm in ((k_new, "k_new"), (v_new, "v_new"), (q, "q")):
-            if t is None and nm == "q":
-                rows.append(None)
-                continue
+        shape = (count, T, H, d)
+        for r, t, nm in zip(self._rows, (k_new, v_new) if q is None else (k_new, v_new, q), ("k_new", "v_new", "q")):
             if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != shape:
                 raise ValueError(f"{nm} must be a bf16 CUDA tensor {list(shape)}")
             st = t.stride()
             tok = st[1]
             if st != (T * tok, tok, d, 1) or tok < H * d:
                 tok = _token_stride(t, nm)
-            rows.append(sva_token_rows(t.data_ptr(), tok))
-        rk, rv, rq = rows
+            r.data, r.token_stride = t.data_ptr(), tok
         if q is not None:
             q_out = q if q_out is None else q_out
             _tok_major(q_out, "q_out", count, T, H, d)
@@ -351,9 +350,10 @@ class Cache:
             if nm == "gamma_q" and gamma_k is not None and gamma_k.dim() != dims:
                 raise ValueError("gamma_k and gamma_q must have the same shape")
             heads = H if dims == 2 else 1
+        rk, rv, rq = self._rows_at
         _check(_lib.sva_rope_kv_write_headnorm(
-            self.handle, arr, count, ctypes.byref(rk), ctypes.byref(rv),
-            ctypes.byref(rq) if rq is not None else None, q_out.data_ptr() if rq is not None else None,
+            self.handle, arr, count, rk, rv, rq if q is not None else None,
+            q_out.data_ptr() if q is not None else None,
             gamma_k.data_ptr() if gamma_k is not None else None,
             gamma_q.data_ptr() if gamma_q is not None else None, heads, float(eps),
             _stream_handle(stream)))
