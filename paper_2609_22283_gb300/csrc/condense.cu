@@ -18,9 +18,8 @@
 // of which the loads 2.0, three cluster barriers 2.4, what passes between the CTAs
 // 2.5, four scans of a block 2.0.  With each digit's eight histograms read by every
 // CTA it was 15.6 us.
-// condense_gather_kernel then copies the kept rows of K and V: bound by HBM (4680 rows
-// of 12 heads of 128, 57 MB, 10.2 us; of 40 heads, 192 MB, 26.9 us: 5.6 and 7.1 TB/s
-// with part of the rows in L2).
+// condense_gather_kernel then copies the kept rows of K and V: bound by HBM (57 MB
+// of the 23.1 us of 28080 candidates of 12 heads, 192 MB of the 45.5 us of 32760 of 40).
 #include <algorithm>
 #include <mutex>
 
@@ -387,42 +386,31 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
   }
 }
 
-// K and V rows of the kept candidates, kRows rows a thread group in flight.
-constexpr int kRows = 4;
-__global__ void __launch_bounds__(256) condense_gather_kernel(const __grid_constant__ CondenseParams p) {
+// K and V rows of the kept candidates, a vector of each a thread: more blocks spread the
+// misses better than several rows a thread in flight (with rows in HBM the whole call on
+// 28080 candidates of 12 heads of 128 takes 23.1 us, with two, three or four rows a thread
+// 26.0 to 26.3; in L2 19.2 against 17.0 to 20.1; 32760 candidates of 40 heads 45.5 against
+// 46.1).  K and V in blocks of their own take 26.9 and 52.2 us.
+constexpr int kCopyThreads = 256;
+__global__ void __launch_bounds__(kCopyThreads) condense_gather_kernel(const __grid_constant__ CondenseParams p) {
   const int vpr = p.d >> 3;  // 16-byte vectors of a row
-  const int groups = 256 / vpr;
-  const int g = threadIdx.x / vpr, c8 = threadIdx.x - g * vpr;
   const int h = blockIdx.y;
-  const int row0 = blockIdx.x * groups * kRows + g;
+  const int row = blockIdx.x * (kCopyThreads / vpr) + threadIdx.x / vpr, c8 = threadIdx.x & (vpr - 1);
   const size_t kv = (size_t)p.H * p.Tpad * p.d;  // elements between K and V of a slot
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
-  uint4 k[kRows], v[kRows];
-  int32_t e[kRows];
-#pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-    const int row = row0 + j * groups;
-    e[j] = row < p.T ? p.index[(size_t)h * p.T + row] : -1;
-  }
-  auto at = [&](int slot, int row) {
-    return static_cast<uint16_t*>(p.pool) + (((size_t)slot * 2 * p.H + h) * p.Tpad + row) * p.d + c8 * 8;
+  if (row >= p.T) return;
+  const int32_t e = p.index[(size_t)h * p.T + row];
+  const int i = e / p.T;
+  auto at = [&](int slot, int r) {
+    return static_cast<uint16_t*>(p.pool) + (((size_t)slot * 2 * p.H + h) * p.Tpad + r) * p.d + c8 * 8;
   };
-#pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-    if (e[j] < 0) continue;
-    const int i = e[j] / p.T;
-    const uint16_t* src = at(p.slot[i], e[j] - i * p.T);
-    k[j] = *reinterpret_cast<const uint4*>(src);
-    v[j] = *reinterpret_cast<const uint4*>(src + kv);
-  }
-#pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-    if (e[j] < 0) continue;
-    uint16_t* dst = at(p.dst, row0 + j * groups);
-    *reinterpret_cast<uint4*>(dst) = k[j];
-    *reinterpret_cast<uint4*>(dst + kv) = v[j];
-  }
+  const uint16_t* src = at(p.slot[i], e - i * p.T);
+  const uint4 k = *reinterpret_cast<const uint4*>(src);
+  const uint4 v = *reinterpret_cast<const uint4*>(src + kv);
+  uint16_t* dst = at(p.dst, row);
+  *reinterpret_cast<uint4*>(dst) = k;
+  *reinterpret_cast<uint4*>(dst + kv) = v;
 }
 
 }  // namespace
@@ -459,8 +447,8 @@ cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s) {
                    log2_cluster > 0 ? 1 << log2_cluster : 0);
   e = cudaLaunchKernelEx(&sel.cfg, select[log2_cluster], p);
   if (e != cudaSuccess) return e;
-  const int rows = 256 / (p.d >> 3) * kRows;
-  LaunchConfig copy(dim3((unsigned)((p.T + rows - 1) / rows), (unsigned)p.H), 256, 0, s);
+  const int rows = kCopyThreads / (p.d >> 3);
+  LaunchConfig copy(dim3((unsigned)((p.T + rows - 1) / rows), (unsigned)p.H), kCopyThreads, 0, s);
   return cudaLaunchKernelEx(&copy.cfg, condense_gather_kernel, p);
 }
 
