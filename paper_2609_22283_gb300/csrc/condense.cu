@@ -19,7 +19,7 @@
 // 2.5, four scans of a block 2.0.  With each digit's eight histograms read by every
 // CTA it was 15.6 us.
 // condense_gather_kernel then copies the kept rows of K and V: bound by HBM (57 MB
-// of the 23.1 us of 28080 candidates of 12 heads, 192 MB of the 45.5 us of 32760 of 40).
+// of the 23.5 us of 28080 candidates of 12 heads, 192 MB of the 46.1 us of 32760 of 40).
 #include <algorithm>
 #include <mutex>
 
@@ -388,16 +388,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
 
 // K and V rows of the kept candidates, a vector of each a thread: more blocks spread the
 // misses better than several rows a thread in flight (with rows in HBM the whole call on
-// 28080 candidates of 12 heads of 128 takes 23.1 us, with two, three or four rows a thread
-// 26.0 to 26.3; in L2 19.2 against 17.0 to 20.1; 32760 candidates of 40 heads 45.5 against
-// 46.1).  K and V in blocks of their own take 26.9 and 52.2 us.
-constexpr int kCopyThreads = 256;
+// 28080 candidates of 12 heads of 128 takes 23.5 us, with two, three or four rows a thread
+// 26.0 to 26.3; 32760 candidates of 40 heads 46.1 either way).  K and V in blocks of their
+// own take 26.9 and 52.2 us.  The next kernel is let in only as blocks end: with its blocks
+// resident earlier, calls in a row take 25.6 us instead of 23.5, in L2 19.6 instead of 17.0
+// (40 heads: 45.6 instead of 46.1).
+constexpr int kCopyThreads = 128;
 __global__ void __launch_bounds__(kCopyThreads) condense_gather_kernel(const __grid_constant__ CondenseParams p) {
   const int vpr = p.d >> 3;  // 16-byte vectors of a row
   const int h = blockIdx.y;
   const int row = blockIdx.x * (kCopyThreads / vpr) + threadIdx.x / vpr, c8 = threadIdx.x & (vpr - 1);
   const size_t kv = (size_t)p.H * p.Tpad * p.d;  // elements between K and V of a slot
-  ptx::pdl_launch_dependents();
   ptx::pdl_wait();
   if (row >= p.T) return;
   const int32_t e = p.index[(size_t)h * p.T + row];
