@@ -52,11 +52,13 @@
 // key tile of the (node, Q tile) pairs that have any visible pair, as far as the tile
 // mask, the frames and the scan of the token masks say, is built first, and only
 // tiles marked for either are loaded and multiplied.  Items that no token mask and no
-// frame cuts are summed as without masks (tile masks with all bits set: 212 us on the
+// frame cuts are summed as without masks (tile masks with all bits set: 205 us on the
 // first case above); elsewhere a warp without a visible pair in its 32 keys x 32
-// queries skips them, and hides scores by the transposed bits where some are visible
+// queries skips them, and leaves out exponentials by the transposed bits where some are visible
 // (4680 queries over own and three history chunks, keys within 6 patch rows and
-// columns: 225 us, of which the scan takes 9; random bits 375).
+// columns: 198 us, of which the scan takes 9; random bits 312; all set 264).  The two
+// blocks of 32 queries are looked at together, so that their transpositions overlap and
+// the sums run through both: one after the other they take 214, 352 and 294 us.
 // All waits are bounded as in the attention kernel; a unit whose CTA gave up one
 // is not written.
 #include <mutex>
@@ -593,6 +595,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     const int q4 = warp & 3;  // TMEM lane quarter this warp may access
     const int row = q4 * 32 + lane;
     const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
+    // bytes of (own, partner's) word that a step of the bits' transposition keeps
+    const uint32_t sel16 = lane & 16 ? 0x3276u : 0x5410u, sel8 = lane & 8 ? 0x3715u : 0x6240u;
     const uint64_t sl2x2 = pair(p.scale_log2, p.scale_log2);
     bool ok = true;
     int n_unit = 0, done = 0, buf = kt;
@@ -656,7 +660,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           if (!ok) break;
         }
         uint64_t acc[4] = {0, 0, 0, 0};
-        // The 16 queries from half * 64 + c * 16 on; with masks those whose bit is set.
+        // The 16 queries from half * 64 + c * 16 on; with masks those whose bit is set (a
+        // test and an addition each: hiding the scores before the exponential instead is two
+        // operations of the integer unit a score, and 5 to 7% slower).
         auto add = [&](const uint32_t (&s)[16], int c, bool some, uint32_t bits) {
           const ulonglong2* nl2 = reinterpret_cast<const ulonglong2*>(&g.nl[half * 64 + c * 16]);
 #pragma unroll
@@ -666,13 +672,23 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
             fma2(x0, x1, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), sl2x2, n.x);
             fma2(x2, x3, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]), sl2x2, n.y);
             if (some) {
-              if (!((bits >> e) & 1u)) x0 = -INFINITY;
-              if (!((bits >> (e + 1)) & 1u)) x1 = -INFINITY;
-              if (!((bits >> (e + 2)) & 1u)) x2 = -INFINITY;
-              if (!((bits >> (e + 3)) & 1u)) x3 = -INFINITY;
+              float a0, a1, b0, b1;
+              unpair(acc[(e >> 1) & 3], a0, a1);
+              unpair(acc[((e >> 1) + 1) & 3], b0, b1);
+              x0 = ex2(x0);
+              x1 = ex2(x1);
+              x2 = ex2(x2);
+              x3 = ex2(x3);
+              if ((bits >> e) & 1u) a0 += x0;
+              if ((bits >> (e + 1)) & 1u) a1 += x1;
+              if ((bits >> (e + 2)) & 1u) b0 += x2;
+              if ((bits >> (e + 3)) & 1u) b1 += x3;
+              acc[(e >> 1) & 3] = pair(a0, a1);
+              acc[((e >> 1) + 1) & 3] = pair(b0, b1);
+            } else {
+              acc[(e >> 1) & 3] = add2(acc[(e >> 1) & 3], pair(ex2(x0), ex2(x1)));
+              acc[((e >> 1) + 1) & 3] = add2(acc[((e >> 1) + 1) & 3], pair(ex2(x2), ex2(x3)));
             }
-            acc[(e >> 1) & 3] = add2(acc[(e >> 1) & 3], pair(ex2(x0), ex2(x1)));
-            acc[((e >> 1) + 1) & 3] = add2(acc[((e >> 1) + 1) & 3], pair(ex2(x2), ex2(x3)));
           }
         };
         uint32_t s0[16], s1[16];
@@ -700,45 +716,86 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         } else {
           const bool worded = kWords && (info & kItemWords), causal = info & kItemCausal;
           const int q0 = (int)(info >> kItemTileShift) * kTile + half * 64;  // this warp's first query
-#pragma unroll
-          for (int c = 0; has_keys && (info & (kItemOn << kt)) && c < 2; ++c) {
+          if (has_keys && (info & (kItemOn << kt))) {
             // this warp's 32 keys for query c * 32 + lane; a query past T, or that saw
             // nothing, adds nothing, whatever its row holds
-            const int q = half * 64 + c * 32 + lane;
-            uint32_t w = worded ? g.word[kWords ? kt * 4 + q4 : 0][kWords ? q : 0] : ~0u;
-            if (g.nl[q] == -INFINITY) w = 0u;
-            uint32_t bits = __ballot_sync(0xffffffffu, w != 0u);  // a bit a query, for this lane's key
-            if (bits == 0u) continue;
-            if (worded && !__all_sync(0xffffffffu, w == ~0u)) {
-              bits = w;  // the 32 x 32 bits transposed
+            uint32_t w[2], bits[2];
+            bool any[2];
 #pragma unroll
-              for (int j = 16; j > 0; j >>= 1) {
-                const uint32_t m = j == 16 ? 0x0000FFFFu : j == 8 ? 0x00FF00FFu : j == 4 ? 0x0F0F0F0Fu
-                                                        : j == 2  ? 0x33333333u
-                                                                  : 0x55555555u;
-                const uint32_t y = __shfl_xor_sync(0xffffffffu, bits, j);
-                bits = (lane & j) ? (bits & ~m) | ((y >> j) & m) : (bits & m) | ((y & m) << j);
+            for (int c = 0; c < 2; ++c) {
+              const int q = half * 64 + c * 32 + lane;
+              w[c] = worded ? g.word[kWords ? kt * 4 + q4 : 0][kWords ? q : 0] : ~0u;
+              if (g.nl[q] == -INFINITY) w[c] = 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              bits[c] = __ballot_sync(0xffffffffu, w[c] != 0u);  // a bit a query, for this lane's key
+              any[c] = bits[c] != 0u;
+            }
+            if (worded && (any[0] || any[1]) && !__all_sync(0xffffffffu, (w[0] & w[1]) == ~0u)) {
+              // the 32 x 32 bits transposed: halves, bytes, then four, two and one of them
+#pragma unroll
+              for (int c = 0; c < 2; ++c) bits[c] = __byte_perm(w[c], __shfl_xor_sync(0xffffffffu, w[c], 16), sel16);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) bits[c] = __byte_perm(bits[c], __shfl_xor_sync(0xffffffffu, bits[c], 8), sel8);
+#pragma unroll
+              for (int j = 4; j > 0; j >>= 1) {
+                const uint32_t m = j == 4 ? 0x0F0F0F0Fu : j == 2 ? 0x33333333u : 0x55555555u;
+                const uint32_t keep = (lane & j) ? ~m : m;
+                const int turn = (lane & j) ? 32 - j : j;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  const uint32_t y = __shfl_xor_sync(0xffffffffu, bits[c], j);
+                  bits[c] = (bits[c] & keep) | (__funnelshift_l(y, y, turn) & ~keep);
+                }
               }
             }
             if (causal) {
-              const int hidden = first_query - (q0 + c * 32);  // queries ahead of the key's frame
-              if (hidden > 0) bits = hidden < 32 ? bits & (~0u << hidden) : 0u;
-              if (!__any_sync(0xffffffffu, bits != 0u)) continue;
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const int hidden = first_query - (q0 + c * 32);  // queries ahead of the key's frame
+                if (hidden > 0) bits[c] = hidden < 32 ? bits[c] & (~0u << hidden) : 0u;
+                any[c] = __any_sync(0xffffffffu, bits[c] != 0u);
+              }
             }
-            const uint32_t col = scol + (uint32_t)(c * 32);
-            tmem_ld16(col, s0);
-            tmem_wait_ld16(s0);
-            // no sum is kept for the keys past the slot's end
-            if (__all_sync(0xffffffffu, bits == ~0u || !mine)) {
+            if (any[0] && any[1]) {
+              // no sum is kept for the keys past the slot's end
+              if (__all_sync(0xffffffffu, (bits[0] & bits[1]) == ~0u || !mine)) {
+                tmem_ld16(scol, s0);
+                tmem_wait_ld16(s0);
+                tmem_ld16(scol + 16, s1);
+                add(s0, 0, false, 0u);
+                tmem_wait_ld16(s1);
+                tmem_ld16(scol + 32, s0);
+                add(s1, 1, false, 0u);
+                tmem_wait_ld16(s0);
+                tmem_ld16(scol + 48, s1);
+                add(s0, 2, false, 0u);
+                tmem_wait_ld16(s1);
+                add(s1, 3, false, 0u);
+              } else {
+                tmem_ld16(scol, s0);
+                tmem_wait_ld16(s0);
+                tmem_ld16(scol + 16, s1);
+                add(s0, 0, true, bits[0]);
+                tmem_wait_ld16(s1);
+                tmem_ld16(scol + 32, s0);
+                add(s1, 1, true, bits[0] >> 16);
+                tmem_wait_ld16(s0);
+                tmem_ld16(scol + 48, s1);
+                add(s0, 2, true, bits[1]);
+                tmem_wait_ld16(s1);
+                add(s1, 3, true, bits[1] >> 16);
+              }
+            } else if (any[0] || any[1]) {
+              const int c = any[0] ? 0 : 1;
+              const uint32_t col = scol + (uint32_t)(c * 32), some = any[0] ? bits[0] : bits[1];
+              tmem_ld16(col, s0);
+              tmem_wait_ld16(s0);
               tmem_ld16(col + 16, s1);
-              add(s0, 2 * c, false, 0u);
+              add(s0, 2 * c, true, some);
               tmem_wait_ld16(s1);
-              add(s1, 2 * c + 1, false, 0u);
-            } else {
-              tmem_ld16(col + 16, s1);
-              add(s0, 2 * c, true, bits);
-              tmem_wait_ld16(s1);
-              add(s1, 2 * c + 1, true, bits >> 16);
+              add(s1, 2 * c + 1, true, some >> 16);
             }
           }
           tc_fence_before();
