@@ -16,7 +16,7 @@
 // memory (with both operands there M = N = 128 needs all of its 128 B a cycle);
 // Q tiles of 128 queries stream past it, for every node that sees the slot.
 //   warp 0     TMA producer: a unit's K tiles, then its Q tiles (4 or 8 stages,
-//              freed by the MMAs' commits);
+//              freed by the MMAs' commits); with masks also the next unit's marks;
 //   warp 2     -lse * log2(e) of a Q tile's rows (-inf past the last row); with
 //              masks also the tile's token words, by copies that need no register;
 //   warps 1, 3 MMA issuers of key tiles 0 and 1;
@@ -48,17 +48,21 @@
 //
 // Launches with fewer units than SMs split a unit's Q tiles over a cluster; the
 // partial sums go to the first CTA's shared memory and are added in rank order.
-// Launches with masks (or frame causality) take one unit a CTA: a bitmap for each
-// key tile of the (node, Q tile) pairs that have any visible pair, as far as the tile
-// mask, the frames and the scan of the token masks say, is built first, and only
-// tiles marked for either are loaded and multiplied.  Items that no token mask and no
-// frame cuts are summed as without masks (tile masks with all bits set: 205 us on the
-// first case above); elsewhere a warp without a visible pair in its 32 keys x 32
+// Launches with masks (or frame causality) have a bitmap for each key tile of a unit,
+// of the (node, Q tile) pairs that have any visible pair as far as the tile mask, the
+// frames and the scan of the token masks say; only tiles marked for either are loaded
+// and multiplied.  Units then differ in work, so the grid has a CTA for each, and a
+// running CTA takes the next that has not started (cluster launch control) and marks
+// its tiles while its own unit's last Q tiles are on their way: the pipeline runs
+// through, and the SMs that are done first take more.  A CTA for each unit instead
+// takes 205 us where that takes 190.  Items that no token mask and no frame cuts are
+// summed as without masks (tile masks with all bits set: 190 us on the first case
+// above); elsewhere a warp without a visible pair in its 32 keys x 32
 // queries skips them, and leaves out exponentials by the transposed bits where some are visible
 // (4680 queries over own and three history chunks, keys within 6 patch rows and
-// columns: 198 us, of which the scan takes 9; random bits 312; all set 264).  The two
+// columns: 189 us, of which the scan takes 9; random bits 299; all set 250).  The two
 // blocks of 32 queries are looked at together, so that their transpositions overlap and
-// the sums run through both: one after the other they take 214, 352 and 294 us.
+// the sums run through both: one after the other they took 16, 35 and 29 us more.
 // All waits are bounded as in the attention kernel; a unit whose CTA gave up one
 // is not written.
 #include <mutex>
@@ -132,7 +136,11 @@ struct Bars {
   uint64_t k_ready[2];        // K tile in TMEM
   uint64_t t_full[2], t_empty[2];  // the second half's sums of a unit
   uint64_t drain;
+  // masks: the marks of the CTA's n-th unit, number n % 2, are there, are no longer read;
+  // the CTA that was taken is known
+  uint64_t m_full[2], m_empty[2], claimed;
 };
+constexpr int kMarkReaders = 3 + 2 * kGroupWarps;  // warps that walk a unit's tiles, but the producer
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -293,6 +301,38 @@ struct Walk {
   }
 };
 
+// Takes a CTA of this launch that has not started: its number goes to `response`, with
+// 16 bytes on `bar`.  Not to be called again once there was none.
+__device__ __forceinline__ void try_cancel(void* response, uint64_t* bar) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the last response has been read
+  mbar_arrive_expect_tx(bar, 16);
+  asm volatile(
+      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+          smem_u32(response)),
+      "r"(smem_u32(bar))
+      : "memory");
+}
+// The CTA that was taken, -1 where there was none.
+__device__ __forceinline__ int canceled_cta(const void* response) {
+  const uint4 r = ld_shared_v4(smem_u32(response));
+  int cta;
+  asm volatile(
+      "{\n"
+      " .reg .b128 h;\n"
+      " .reg .b64 lo, hi;\n"
+      " .reg .pred p;\n"
+      " mov.b64 lo, {%1, %2};\n"
+      " mov.b64 hi, {%3, %4};\n"
+      " mov.b128 h, {lo, hi};\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n"
+      " mov.s32 %0, -1;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, h;\n"
+      "}\n"
+      : "=&r"(cta)
+      : "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w));
+  return cta;
+}
+
 struct Unit {
   int si, h, kp;  // index of the slot in the launch's list, head, pair of key tiles
 };
@@ -322,8 +362,14 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
   __shared__ Stage<kWords> stage[kRing];
-  __shared__ uint32_t marks[2][kMask ? kMarkWords : 1];
-  __shared__ float part[kMaxWeightSplit][2 * kTile];  // rank 0: the cluster's partial sums
+  __shared__ uint32_t marks[2][2][kMask ? kMarkWords : 1];  // of the CTA's units, by turns
+  __shared__ int unit_sh[2];                                // their numbers, -1 after the last
+  __shared__ uint4 response;
+  // rank 0: the cluster's partial sums; a cluster takes one unit, with masks they lie on
+  // the second unit's marks
+  __shared__ float part_sh[kMask ? 1 : kMaxWeightSplit][2 * kTile];
+  static_assert(!kMask || sizeof(marks[1]) == sizeof(float) * kMaxWeightSplit * 2 * kTile, "part");
+  float (*part)[2 * kTile] = kMask ? reinterpret_cast<float (*)[2 * kTile]>(marks[1]) : part_sh;
   __shared__ float half_sum[2][kTile];                // the second half's sums of a unit
   __shared__ volatile float part_lost;                // rank 0: a CTA of the cluster gave up
 
@@ -331,9 +377,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   const int lane = threadIdx.x & 31;
   const int ns = p.n_split;
   const int rank = ns > 1 ? (int)blockIdx.x % ns : 0;
-  // units of this CTA: u0, u0 + u_step, ...
+  // units of this CTA: u0, u0 + u_step, ...; with masks u0, and those of the CTAs it takes
   const int u0 = ns > 1 ? (int)blockIdx.x / ns : (int)blockIdx.x;
-  const int u_step = ns > 1 ? p.units : (int)gridDim.x;  // masked launches: one unit a CTA
+  const int u_step = ns > 1 ? p.units : (int)gridDim.x;
   const uint64_t tmo = p.timeout_ns;
 
   pdl_launch_dependents();
@@ -360,7 +406,11 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       mbar_init(&bars.k_ready[k], kGroupWarps);
       mbar_init(&bars.t_full[k], kGroupWarps / 2 * 32);
       mbar_init(&bars.t_empty[k], kGroupWarps / 2 * 32);
+      mbar_init(&bars.m_full[k], 1);
+      mbar_init(&bars.m_empty[k], kMarkReaders);
     }
+    mbar_init(&bars.claimed, 1);
+    unit_sh[0] = u0;
     mbar_init(&bars.drain, 2);
     fence_mbar_init();
   }
@@ -369,38 +419,38 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     tmem_relinquish();
   }
   pdl_wait();  // everything above is this CTA's own; what follows reads and writes global memory
-  if constexpr (kMask) {
-    // Which Q tiles have anything visible of either key tile of this unit, by the tile
-    // mask, the frames and the scan of the token masks.
-    const Unit un = unit_of(p, u0);
-    const int n_ref = p.first[un.si + 1] - p.first[un.si];
-    const int n_all = n_ref * p.n_qt;
-    for (int base = warp * 32; base < n_all; base += kThreads) {
-      const int i = base + lane;
-      bool on[2] = {false, false};
-      if (i < n_all) {
-        const int r = i / p.n_qt, qt = i - r * p.n_qt;
-        const uint32_t ref = p.ref[p.first[un.si] + r];
-        const int state = (ref >> kRefStateShift) & 31;
-        const size_t qrow = (size_t)(ref & 63) * p.n_qt + qt;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const int t = 2 * un.kp + kt, k = state * p.n_qt + t;
-          on[kt] = t < p.n_qt;
-          if (on[kt] && p.tile_mask) on[kt] = (p.tile_mask[qrow * p.mask_words + (k >> 5)] >> (k & 31)) & 1u;
-          if (on[kt] && p.any_tile) on[kt] = p.any_tile[qrow * p.any_stride + k] != 0;
-          if (on[kt] && state == 0 && (ref & kRefCausal)) {
-            const int last = min((qt + 1) * kTile, p.T) - 1;
-            on[kt] = last / p.frame_tokens >= t * kTile / p.frame_tokens;
-          }
-        }
-      }
+  auto tiles_of = [&](const Unit& un) { return (p.first[un.si + 1] - p.first[un.si]) * p.n_qt; };  // < 2^16
+  // Which Q tiles have anything visible of either key tile of a unit, by the tile mask,
+  // the frames and the scan of the token masks: of 32 tiles, a lane's each.
+  auto mark = [&](const Unit& un, uint32_t (&to)[2][kMask ? kMarkWords : 1], int base) {
+    const int i = base + lane;
+    bool on[2] = {false, false};
+    if (i < tiles_of(un)) {
+      const int r = i / p.n_qt, qt = i - r * p.n_qt;
+      const uint32_t ref = p.ref[p.first[un.si] + r];
+      const int state = (ref >> kRefStateShift) & 31;
+      const size_t qrow = (size_t)(ref & 63) * p.n_qt + qt;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
-        const uint32_t m = __ballot_sync(0xffffffffu, on[kt]);
-        if (lane == 0) marks[kt][base >> 5] = m;
+        const int t = 2 * un.kp + kt, k = state * p.n_qt + t;
+        on[kt] = t < p.n_qt;
+        if (on[kt] && p.tile_mask) on[kt] = (p.tile_mask[qrow * p.mask_words + (k >> 5)] >> (k & 31)) & 1u;
+        if (on[kt] && p.any_tile) on[kt] = p.any_tile[qrow * p.any_stride + k] != 0;
+        if (on[kt] && state == 0 && (ref & kRefCausal)) {
+          const int last = min((qt + 1) * kTile, p.T) - 1;
+          on[kt] = last / p.frame_tokens >= t * kTile / p.frame_tokens;
+        }
       }
     }
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const uint32_t m = __ballot_sync(0xffffffffu, on[kt]);
+      if (lane == 0) to[kt][base >> 5] = m;
+    }
+  };
+  if constexpr (kMask) {
+    const Unit un = unit_of(p, u0);
+    for (int base = warp * 32; base < tiles_of(un); base += kThreads) mark(un, marks[0], base);
   }
   tc_fence_before();
   __syncthreads();
@@ -408,46 +458,114 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
   if (ns > 1) cluster_sync();  // every CTA of the cluster runs, its part_lost is clear
   const uint32_t tbase = tmem_base_sh;
 
-  // The Q tiles [begin, end) of a unit that this CTA takes.
-  auto walk_of = [&](const Unit& un) {
+  // The Q tiles [begin, end) of the CTA's n-th unit that it takes.
+  auto walk_of = [&](const Unit& un, int n) {
     const uint32_t n_all = (uint32_t)(p.first[un.si + 1] - p.first[un.si]) * (uint32_t)p.n_qt;  // < 2^16
     uint32_t begin = 0, end = n_all;
     if (ns > 1) {
       begin = n_all * (uint32_t)rank / (uint32_t)ns;
       end = n_all * (uint32_t)(rank + 1) / (uint32_t)ns;
     }
-    return Walk<kMask>(marks, (int)begin, (int)end, p.n_qt);
+    return Walk<kMask>(marks[kMask ? n & 1 : 0], (int)begin, (int)end, p.n_qt);
+  };
+  // The CTA's n-th unit, after `u`; -1 past the last, or where a wait expired (`ok`).
+  auto unit_after = [&](int u, int n, bool& ok) {
+    if constexpr (kMask) {
+      ok = mbar_wait(&bars.m_full[n & 1], (uint32_t)(n >> 1) & 1u, &abort_flag, tmo);
+      ok = __all_sync(0xffffffffu, ok);
+      return ok ? unit_sh[n & 1] : -1;
+    } else {
+      return u + u_step < p.units ? u + u_step : -1;
+    }
+  };
+  // This warp reads the marks of the n-th unit no more.
+  auto walked = [&](int n) {
+    if constexpr (kMask) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.m_empty[n & 1]);
+    }
   };
 
   int q_issued = 0, k_issued = 0;  // producer: copies started
   if (warp == 0) {
     // ------------------------------------------------------------ producer
-    if (lane == 0) {
+    // One lane; with masks the warp, which also takes and marks the next unit.
+    if (kMask || lane == 0) {
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        const bool there = mbar_wait(bar, parity, &abort_flag, tmo);
+        return kMask ? __all_sync(0xffffffffu, there) != 0 : there;
+      };
+      const bool first_lane = lane == 0;
       bool ok = true;
-      for (int u = u0; ok && u < p.units; u += u_step) {
+      if (kMask && first_lane) mbar_arrive(&bars.m_full[0]);  // the first unit's marks are there
+      for (int u = u0, n = 0; u >= 0; ++n) {
         const Unit un = unit_of(p, u);
         const int row = ((p.slot[un.si] * 2) * p.H + un.h) * p.Tpad + un.kp * 2 * kTile;
         const bool two = 2 * un.kp + 1 < p.n_qt;
-        ok = mbar_wait(&bars.k_empty, ((uint32_t)k_issued & 1u) ^ 1u, &abort_flag, tmo);
+        ok = wait(&bars.k_empty, ((uint32_t)k_issued & 1u) ^ 1u);
         if (!ok) break;
-        mbar_arrive_expect_tx(&bars.k_full, (two ? 2 : 1) * C::kTileBytes);
+        if (first_lane) {
+          mbar_arrive_expect_tx(&bars.k_full, (two ? 2 : 1) * C::kTileBytes);
 #pragma unroll
-        for (int b = 0; b < C::kBoxes; ++b) {
-          tma_load_2d(smem + C::kOffK + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full, b * 64, row);
-          if (two)
-            tma_load_2d(smem + C::kOffK + C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full, b * 64,
-                        row + kTile);
+          for (int b = 0; b < C::kBoxes; ++b) {
+            tma_load_2d(smem + C::kOffK + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full, b * 64, row);
+            if (two)
+              tma_load_2d(smem + C::kOffK + C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full, b * 64,
+                          row + kTile);
+          }
         }
         ++k_issued;
-        Walk<kMask> walk = walk_of(un);
+        Walk<kMask> walk = walk_of(un, n);
+        // The next unit: a CTA that has not started is taken when few tiles are left to load
+        // (late enough that an SM that is done earlier gets it), then 32 of its tiles are
+        // marked with every tile loaded: the Q tiles in flight hide that.
+        int next = -1, at = 0;   // its number, the next tile to mark
+        int left = 0, early = 0;
+        enum { kLater, kClaimed, kMarking, kDone } step = kLater;
+        if constexpr (kMask) {
+          left = walk.count();
+          early = 4 + (tiles_of(un) >> 5);
+        }
+        // The unit whose marks are to be free: the one before; or this one where it has no tile
+        // (no S makes the sums wait for the MMA warps then, and k_ready has one phase).
+        const int free = left == 0 ? n : n - 1;
+        auto advance = [&]() {
+          if (step == kLater) {
+            if (ns == 1 && first_lane) try_cancel(&response, &bars.claimed);
+            step = kClaimed;
+          } else if (step == kClaimed) {
+            if (ns == 1) {
+              const int zero = 0;  // the response is waited for in any case
+              ok = __all_sync(0xffffffffu, mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo)) != 0;
+              if (ok) next = canceled_cta(&response);
+            }
+            ok = ok && wait(&bars.m_empty[free & 1], (uint32_t)(free >> 1) & 1u);
+            step = kMarking;
+          } else {
+            if (next >= 0 && at < tiles_of(unit_of(p, next))) {
+              mark(unit_of(p, next), marks[(n + 1) & 1], at);
+              at += 32;
+              return;
+            }
+            if (first_lane) {
+              unit_sh[(n + 1) & 1] = next;
+              mbar_arrive(&bars.m_full[(n + 1) & 1]);
+            }
+            step = kDone;
+          }
+        };
         int r, qt;
         while (walk.next(r, qt)) {
+          if constexpr (kMask) {
+            if (left-- <= early && step != kDone) advance();
+            if (!ok) break;
+          }
           const int node = p.ref[p.first[un.si] + r] & 63;
           const int st = q_issued % C::kStages;
-          ok = mbar_wait(&bars.q_empty[st], ((uint32_t)(q_issued / C::kStages) & 1u) ^ 1u, &abort_flag, tmo);
+          ok = wait(&bars.q_empty[st], ((uint32_t)(q_issued / C::kStages) & 1u) ^ 1u);
           if (!ok) break;
           // fault_mode 2 (test hook): withhold the copy of the second tile
-          if (!(p.fault_mode == 2 && q_issued == 1)) {
+          if (first_lane && !(p.fault_mode == 2 && q_issued == 1)) {
             mbar_arrive_expect_tx(&bars.q_full[st], C::kTileBytes);
 #pragma unroll
             for (int b = 0; b < C::kBoxes; ++b)
@@ -456,24 +574,36 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
           }
           ++q_issued;
         }
+        if constexpr (kMask) {
+          while (ok && step != kDone) advance();
+          u = next;
+        } else {
+          u = unit_after(u, n + 1, ok);
+        }
+        if (!ok) {
+          const int zero = 0;  // no response outlives the CTA
+          if (kMask && ns == 1 && step == kClaimed) mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo);
+          break;
+        }
       }
-      if (!ok) record_timeout(p, &abort_flag);
+      if (!ok && first_lane) record_timeout(p, &abort_flag);
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------ log-sum-exps
     // Loaded an item ahead of their stage.
-    int u = u0;
-    Unit un = unit_of(p, u < p.units ? u : 0);
-    Walk<kMask> walk = walk_of(un);
+    bool ok = true;
+    int u = u0, n = 0;
+    Unit un = unit_of(p, u);
+    Walk<kMask> walk = walk_of(un, n);
     float v[4];  // of queries k * 32 + lane
     int r = 0, qt = 0;
     auto load = [&]() {  // the next item's; false past the last
-      if (u >= p.units) return false;
       while (!walk.next(r, qt)) {
-        u += u_step;
-        if (u >= p.units) return false;
+        walked(n);
+        u = unit_after(u, ++n, ok);
+        if (u < 0) return false;
         un = unit_of(p, u);
-        walk = walk_of(un);
+        walk = walk_of(un, n);
       }
       const int node = p.ref[p.first[un.si] + r] & 63;
       const float* src = p.lse + ((size_t)node * p.H + un.h) * p.T;
@@ -523,7 +653,6 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
                  (causal ? kItemCausal : 0u) | (uint32_t)qt << kItemTileShift;
       if constexpr (kWords) cp_async_arrive(&g.l_full);
     };
-    bool ok = true;
     bool more = load();
     Ring it;
     while (more) {
@@ -557,9 +686,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     bool reused = false;        // there was one
     int ahead = kt == 1 ? 1 : 2;  // items until then
     int buf = kt;               // S buffer of step 2 * it + kt
-    for (int u = u0; ok && u < p.units; u += u_step, ++n_unit) {
+    for (int u = u0; ok && u >= 0;) {
       const Unit un = unit_of(p, u);
-      Walk<kMask> walk = walk_of(un);
+      Walk<kMask> walk = walk_of(un, n_unit);
       ok = wait(&bars.k_ready[kt], (uint32_t)n_unit & 1u);
       if (!ok) break;
       int r, qt;
@@ -586,6 +715,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         buf = buf == 0 ? 2 : buf - 1;  // two steps on, modulo 3
         it.step();
       }
+      if (!ok) break;
+      walked(n_unit);
+      u = unit_after(u, ++n_unit, ok);
     }
     if (!ok && lane == 0) record_timeout(p, &abort_flag);
   } else {
@@ -626,8 +758,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       ++n_unit;
       return true;
     };
-    if (u0 < p.units) ok = copy_k();
-    for (int u = u0; ok && u < p.units; u += u_step) {
+    ok = copy_k();
+    for (int u = u0; ok && u >= 0;) {
       const Unit un = unit_of(p, u);
       const int key = (un.kp * 2 + kt) * kTile + row;
       const size_t at = ((size_t)p.slot[un.si] * p.H + un.h) * p.T + key;
@@ -635,13 +767,17 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       const bool has_keys = key - lane < p.T;  // the warp's part of the tile (K is not loaded past the slot)
       const float before = ld_f32_if(p.prev + at, p.prev != nullptr && mine && ns == 1, 0.0f);
       float total = 0.0f;
-      const bool next_k = u + u_step < p.units;  // another unit's K is to follow
-      Walk<kMask> walk = walk_of(un);
-      int left = walk.count();
-      if (left == 0 && next_k) {  // no Q tile (masks only): nothing reads this K
-        ok = copy_k();
-        if (!ok) break;
-      }
+      int left = walk_of(un, done).count();
+      walked(done);
+      int next = kMask ? -1 : unit_after(u, done + 1, ok);
+      // The unit's last S is complete, or it has none (masks only): no MMA reads its K any
+      // more, and the next unit's follows.
+      auto next_k = [&]() {
+        if constexpr (kMask) next = unit_after(u, done + 1, ok);
+        if (next >= 0) ok = copy_k();
+        return ok;
+      };
+      if (left == 0 && !next_k()) break;
       const int first_query = key / p.frame_tokens * p.frame_tokens;  // that sees this key under frame causality
       while (left > 0) {
         Stage<kWords>& g = stage[it.at];
@@ -655,10 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         }
         tc_fence_after();
         --left;
-        if (left == 0 && next_k) {  // the unit's last S is complete: no MMA reads its K any more
-          ok = copy_k();
-          if (!ok) break;
-        }
+        if (left == 0 && !next_k()) break;
         uint64_t acc[4] = {0, 0, 0, 0};
         // The 16 queries from half * 64 + c * 16 on; with masks those whose bit is set (a
         // test and an addition each: hiding the scores before the exponential instead is two
@@ -831,6 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         }
       }
       ++done;
+      u = next;
     }
     if (!ok) {
       if (lane == 0) {

@@ -263,6 +263,29 @@ def test_masked_cluster_split(sva_mod):
     c.close()
 
 
+@pytest.mark.parametrize("d,causal,tokens", [(128, False, False), (64, True, False), (64, False, True), (128, True, True)])
+def test_more_masked_units_than_sms(sva_mod, d, causal, tokens):
+    """600 units that differ in work, some with none at all: each is summed once, whichever CTA takes it."""
+    c = Case(sva_mod, 4, 5, 55, 20, d, _chain(2, 3), causal=causal)
+    T, n, nt = c.T, 2, 9
+    tile = torch.rand((n, nt, 4 * nt), generator=c.g, device="cuda") < torch.linspace(0.05, 1.0, 4 * nt, device="cuda")
+    tile[:, :, 2:4] = False                 # the second pair of the own chunk's key tiles
+    tile[:, :, nt:2 * nt] = False           # the first history state of either node
+    own = hist = None
+    if tokens:
+        own = torch.rand((n, T, T), generator=c.g, device="cuda") < 0.5
+        hist = torch.rand((n, T, 3, T), generator=c.g, device="cuda") < 0.5
+        hist[:, 100:700, 1] = False
+    first = c.check(tile=tile, own=own, hist=hist)
+    masks = dict(tile_mask=_pack(tile), own_mask=_pack(own) if tokens else None, hist_mask=_pack(hist) if tokens else None)
+    for _ in range(20):
+        again = torch.full(c.shape, -7.0, device="cuda")
+        c.cache.attend_weights(c.nodes, c.q, c.lse, again, **masks)
+        assert torch.equal(again, first)
+    assert c.cache.poll() == sva_mod.OK
+    c.close()
+
+
 def test_hidden_keys_may_hold_anything(sva_mod):
     """NaN and infinities in keys that no query sees: zero for them, and the others as without."""
     c = Case(sva_mod, 1, 10, 33, 2, 128, _chain(1, 1))
