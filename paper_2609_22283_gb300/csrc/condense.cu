@@ -2,8 +2,8 @@
 // tokens of n states, each head keeps the T whose weight is largest, in their
 // order, as one state.
 //
-// Two launches.  condense_select_kernel finds which: a cluster of up to eight
-// CTAs per head, each with a contiguous range of the head's candidates in shared
+// Two launches, one for the smallest states.  condense_select_kernel finds which: a
+// cluster of up to eight CTAs per head, each with a contiguous range of the head's candidates in shared
 // memory, finds the T-th largest key (the weights as integers of the same order)
 // digit by digit, 11, 11 and 10 bits.  The first digit's histogram has few bins in
 // use; each CTA adds its own to every CTA's sums through distributed shared
@@ -132,6 +132,22 @@ __device__ __forceinline__ Digit find_digit(uint4 bins, int need, uint32_t* warp
   }
   __syncthreads();
   return *found;
+}
+
+// Vector c8 of K and of V of head h's kept candidate `row`.
+__device__ __forceinline__ void copy_vector(const CondenseParams& p, int h, int row, int c8) {
+  const size_t kv = (size_t)p.H * p.Tpad * p.d;  // elements between K and V of a slot
+  const int32_t e = p.index[(size_t)h * p.T + row];
+  const int i = e / p.T;
+  auto at = [&](int slot, int r) {
+    return static_cast<uint16_t*>(p.pool) + (((size_t)slot * 2 * p.H + h) * p.Tpad + r) * p.d + c8 * 8;
+  };
+  const uint16_t* src = at(p.slot[i], e - i * p.T);
+  const uint4 k = *reinterpret_cast<const uint4*>(src);
+  const uint4 v = *reinterpret_cast<const uint4*>(src + kv);
+  uint16_t* dst = at(p.dst, row);
+  *reinterpret_cast<uint4*>(dst) = k;
+  *reinterpret_cast<uint4*>(dst + kv) = v;
 }
 
 // kCluster CTAs a head.
@@ -383,6 +399,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
   if constexpr (kCluster > 1) {
     __syncwarp();
     cluster_wait();
+  } else if (p.copy) {
+    __syncthreads();
+    const int vpr = p.d >> 3;
+    for (int v = tid; v < p.T * vpr; v += kSelThreads) copy_vector(p, h, v / vpr, v & (vpr - 1));
   }
 }
 
@@ -396,22 +416,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) condense_select_kernel(const _
 constexpr int kCopyThreads = 128;
 __global__ void __launch_bounds__(kCopyThreads) condense_gather_kernel(const __grid_constant__ CondenseParams p) {
   const int vpr = p.d >> 3;  // 16-byte vectors of a row
-  const int h = blockIdx.y;
-  const int row = blockIdx.x * (kCopyThreads / vpr) + threadIdx.x / vpr, c8 = threadIdx.x & (vpr - 1);
-  const size_t kv = (size_t)p.H * p.Tpad * p.d;  // elements between K and V of a slot
+  const int row = blockIdx.x * (kCopyThreads / vpr) + threadIdx.x / vpr;
   ptx::pdl_wait();
-  if (row >= p.T) return;
-  const int32_t e = p.index[(size_t)h * p.T + row];
-  const int i = e / p.T;
-  auto at = [&](int slot, int r) {
-    return static_cast<uint16_t*>(p.pool) + (((size_t)slot * 2 * p.H + h) * p.Tpad + r) * p.d + c8 * 8;
-  };
-  const uint16_t* src = at(p.slot[i], e - i * p.T);
-  const uint4 k = *reinterpret_cast<const uint4*>(src);
-  const uint4 v = *reinterpret_cast<const uint4*>(src + kv);
-  uint16_t* dst = at(p.dst, row);
-  *reinterpret_cast<uint4*>(dst) = k;
-  *reinterpret_cast<uint4*>(dst + kv) = v;
+  if (row < p.T) copy_vector(p, blockIdx.y, row, threadIdx.x & (vpr - 1));
 }
 
 }  // namespace
@@ -446,8 +453,12 @@ cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s) {
   p.hold = per <= kHeldKeys ? 1 : 0;
   LaunchConfig sel(dim3((unsigned)(p.H << log2_cluster)), kSelThreads, (size_t)((p.hold ? per : 0) + std::min(per, kListKeys)) * 4, s,
                    log2_cluster > 0 ? 1 << log2_cluster : 0);
+  // Up to two vectors a thread are copied where they are selected: 64 tokens of 12 heads
+  // of 128 from four states take 5.8 us a call then, 6.7 with a second launch (in a graph
+  // 5.6 and 5.2; one token of two states 4.8 and 6.5, 3.9 and 4.7), 128 tokens 6.9 and 6.6.
+  p.copy = log2_cluster == 0 && p.T * (p.d >> 3) <= 2 * kSelThreads ? 1 : 0;
   e = cudaLaunchKernelEx(&sel.cfg, select[log2_cluster], p);
-  if (e != cudaSuccess) return e;
+  if (p.copy || e != cudaSuccess) return e;
   const int rows = kCopyThreads / (p.d >> 3);
   LaunchConfig copy(dim3((unsigned)((p.T + rows - 1) / rows), (unsigned)p.H), kCopyThreads, 0, s);
   return cudaLaunchKernelEx(&copy.cfg, condense_gather_kernel, p);

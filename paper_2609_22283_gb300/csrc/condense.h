@@ -12,10 +12,11 @@ struct CondenseParams {
   int32_t T, Tpad, H, d;
   int32_t n_src, dst;
   int32_t hold;     // 1: a CTA's keys stay in shared memory
+  int32_t copy;     // 1: the selection copies the rows too
   int32_t slot[SVA_MAX_CTX];
 };
 
-// Sets p.hold.
+// Sets p.hold and p.copy.
 cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s);
 
 }  // namespace sva

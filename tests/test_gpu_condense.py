@@ -74,6 +74,17 @@ def test_random_weights(sva_mod, F, Hp, Wp, H, d, n):
     c.close()
 
 
+@pytest.mark.parametrize("F,Hp,Wp,H,d,n", [(1, 8, 16, 3, 64, 16), (1, 3, 43, 3, 64, 15), (1, 8, 8, 3, 128, 16),
+                                           (1, 5, 13, 3, 128, 16), (1, 1, 2, 40, 128, 2), (2, 3, 7, 12, 64, 5)])
+def test_small_states(sva_mod, F, Hp, Wp, H, d, n):
+    """Rows copied by the selection (up to 128 tokens of 64, 64 of 128) and by a launch of their own, ties among them."""
+    T = F * Hp * Wp
+    c, src, dst, g = _cache(sva_mod, F, Hp, Wp, H, d, n)
+    w = torch.floor(3 * torch.rand((n + 2, H, T), generator=g, device="cuda"))
+    _check(c, src, dst, w, T, H)
+    c.close()
+
+
 @pytest.mark.parametrize("kind", ["zeros", "equal", "few", "signs", "nan", "all nan", "inf", "close", "subnormal", "line"])
 def test_ties_and_odd_values(sva_mod, kind):
     """Equal weights go to the lowest candidates, over CTA borders too (2214 candidates a CTA)."""
