@@ -1391,6 +1391,9 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
   p.n_split = (int32_t)std::max(1ll, std::min({(long long)sva::kMaxWeightSplit, c->num_sms / units, tiles / 2}));
   long long grid = units * p.n_split;
   if (!p.masked && p.n_split == 1) grid = std::min<long long>(units, c->num_sms);
+  // Masked units differ in work: CTAs that are done take others'.  (Where all run at
+  // once asking for another costs 0.1 to 0.5 us.)
+  p.take = p.masked && units > c->num_sms ? 1 : 0;
   // Token masks are scanned for the tiles they leave anything of where the walk of
   // all tiles is about as long as that of the attention's rule: a Q tile past a pair
   // of key tiles takes about 0.9 us.

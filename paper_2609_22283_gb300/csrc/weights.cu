@@ -411,6 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
     }
     mbar_init(&bars.claimed, 1);
     unit_sh[0] = u0;
+    unit_sh[1] = -1;
     mbar_init(&bars.drain, 2);
     fence_mbar_init();
   }
@@ -497,7 +498,11 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
       };
       const bool first_lane = lane == 0;
       bool ok = true;
-      if (kMask && first_lane) mbar_arrive(&bars.m_full[0]);  // the first unit's marks are there
+      const bool takes = kMask && p.take != 0;
+      if (kMask && first_lane) {
+        mbar_arrive(&bars.m_full[0]);  // the first unit's marks are there
+        if (!takes) mbar_arrive(&bars.m_full[1]);  // and no unit follows
+      }
       for (int u = u0, n = 0; u >= 0; ++n) {
         const Unit un = unit_of(p, u);
         const int row = ((p.slot[un.si] * 2) * p.H + un.h) * p.Tpad + un.kp * 2 * kTile;
@@ -521,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         // marked with every tile loaded: the Q tiles in flight hide that.
         int next = -1, at = 0;   // its number, the next tile to mark
         int left = 0, early = 0;
-        enum { kLater, kClaimed, kMarking, kDone } step = kLater;
+        enum { kLater, kClaimed, kMarking, kDone } step = takes ? kLater : kDone;
         if constexpr (kMask) {
           left = walk.count();
           early = 4 + (tiles_of(un) >> 5);
@@ -531,14 +536,12 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         const int free = left == 0 ? n : n - 1;
         auto advance = [&]() {
           if (step == kLater) {
-            if (ns == 1 && first_lane) try_cancel(&response, &bars.claimed);
+            if (first_lane) try_cancel(&response, &bars.claimed);
             step = kClaimed;
           } else if (step == kClaimed) {
-            if (ns == 1) {
-              const int zero = 0;  // the response is waited for in any case
-              ok = __all_sync(0xffffffffu, mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo)) != 0;
-              if (ok) next = canceled_cta(&response);
-            }
+            const int zero = 0;  // the response is waited for in any case
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo)) != 0;
+            if (ok) next = canceled_cta(&response);
             ok = ok && wait(&bars.m_empty[free & 1], (uint32_t)(free >> 1) & 1u);
             step = kMarking;
           } else {
@@ -582,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const __grid_const
         }
         if (!ok) {
           const int zero = 0;  // no response outlives the CTA
-          if (kMask && ns == 1 && step == kClaimed) mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo);
+          if (kMask && step == kClaimed) mbar_wait(&bars.claimed, (uint32_t)n & 1u, &zero, tmo);
           break;
         }
       }

@@ -38,6 +38,7 @@ struct alignas(128) WeightParams {
   const uint8_t* any_tile;
   int32_t any_stride;
   int32_t masked;       // some mask, or a frame-causal node
+  int32_t take;     // 1: a masked launch's CTAs take units of CTAs that have not started
   // The distinct slots that the nodes see, those seen by most nodes first, and
   // for slot i the nodes that see it: refs [first[i], first[i + 1]).
   int32_t n_slots;

@@ -286,6 +286,24 @@ def test_more_masked_units_than_sms(sva_mod, d, causal, tokens):
     c.close()
 
 
+def test_masked_units_in_a_graph(sva_mod):
+    """A captured masked launch with more units than SMs gives the direct call's bits at every replay."""
+    c = Case(sva_mod, 2, 14, 20, 24, 64, _chain(1, 3), causal=True)
+    tile = torch.rand((1, 5, 20), generator=c.g, device="cuda") < 0.6
+    direct = c.check(tile=tile)
+    packed = _pack(tile)
+    out = torch.full(c.shape, -7.0, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.attend_weights(c.nodes, c.q, c.lse, out, tile_mask=packed)
+    for _ in range(5):
+        out.fill_(-7.0)
+        graph.replay()
+        assert torch.equal(out, direct)
+    assert c.cache.poll() == sva_mod.OK
+    c.close()
+
+
 def test_hidden_keys_may_hold_anything(sva_mod):
     """NaN and infinities in keys that no query sees: zero for them, and the others as without."""
     c = Case(sva_mod, 1, 10, 33, 2, 128, _chain(1, 1))
