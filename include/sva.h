@@ -376,10 +376,11 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
  *   prev   [num_slots][H][T] fp32, or NULL: nothing before (decay is then not used)
  *   decay  0..1
  *   out    [num_slots][H][T] fp32; only the slots that some node sees are written.
- *          May be prev itself, otherwise shares no memory with it
+ *          May be prev itself, otherwise shares no memory with it; shares none with
+ *          q, lse or a mask
  * fp32 throughout (the products of bf16 accumulate in fp32); the same inputs give
  * the same bits.  Stream-ordered.  Errors: as sva_attend_nodes_masked, plus
- * INVALID_ARGUMENT for decay. */
+ * INVALID_ARGUMENT for decay or an overlapping out. */
 sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
                               const float* lse, float scale, const sva_attn_mask* mask,
                               const float* prev, float decay, float* out, sva_stream s);

@@ -52,6 +52,12 @@ sva_status cuda_fail(cudaError_t e, const char* what) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Do two ranges of memory have a byte in common?  NULL is no range.
+bool share_memory(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  return a != nullptr && b != nullptr && a0 < b0 + b_bytes && b0 < a0 + a_bytes;
+}
+
 // True when `p` points into device memory of `device`.
 bool on_device(const void* p, int device) {
   cudaPointerAttributes attr;
@@ -1316,6 +1322,25 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
   const sva_attn_mask m = mask != nullptr ? *mask : sva_attn_mask{};
   st = check_masks(c, nodes, n_nodes, m);
   if (st != SVA_OK) return st;
+  // Sums are written while other CTAs still read: only prev, which the thread that
+  // writes a sum reads itself, may be where out is.
+  const size_t tokens = (size_t)n_nodes * c->L.T, rows = (size_t)n_nodes * (c->L.Tpad / sva::kTile);
+  const size_t sums = (size_t)g.num_slots * g.num_heads * c->L.T * sizeof(float);
+  const size_t hist_row = std::min((size_t)m.hist_states * (size_t)m.hist_words, (size_t)1 << 40);
+  const struct {
+    const char* name;
+    const void* data;
+    size_t bytes;
+  } inputs[] = {{"q", q, tokens * g.num_heads * g.head_dim * 2},
+                {"lse", lse, tokens * g.num_heads * sizeof(float)},
+                {"prev", prev != out ? prev : nullptr, sums},
+                {"tile_mask", m.tile_mask, m.tile_mask ? rows * m.tile_words * 4 : 0},
+                {"own_mask", m.own_mask, m.own_mask ? tokens * m.own_words * 4 : 0},
+                {"hist_mask", m.hist_mask, m.hist_mask ? tokens * hist_row * 4 : 0}};
+  for (const auto& in : inputs)
+    if (share_memory(out, sums, in.data, in.bytes))
+      return fail(SVA_ERR_INVALID_ARGUMENT, "out shares memory with %s (it may be prev itself, and nothing else)",
+                  in.name);
 
   static thread_local sva::WeightParams p;
   std::memset(&p, 0, sizeof(p));
