@@ -399,7 +399,8 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
  *             whose chunk is not before any source's (so that Eq. 4's causality
  *             holds for what it contains)
  *   weight    [num_slots][H][T] fp32, as sva_attend_weights accumulates it
- *   index     [H][T] int32, receives the kept candidates in ascending order
+ *   index     [H][T] int32, receives the kept candidates in ascending order; shares
+ *             no memory with weight
  * Stream-ordered.  Errors: INVALID_ARGUMENT, NOT_RESIDENT (a source), CAUSALITY (a
  * source of another sequence or after the destination's chunk), CAPACITY (n_src),
  * CUDA. */

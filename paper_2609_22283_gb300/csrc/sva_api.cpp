@@ -1452,6 +1452,10 @@ sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_s
   if (dst_slot < 0 || dst_slot >= g.num_slots || !c->slots[dst_slot].bound)
     return fail(SVA_ERR_INVALID_ARGUMENT, "dst_slot %d is not a bound slot", dst_slot);
   const SlotInfo& dst = c->slots[dst_slot];
+  // a CTA writes its kept candidates while others may still read weights
+  const size_t row_bytes = (size_t)g.num_heads * c->L.T * 4;
+  if (share_memory(index, row_bytes, weight, g.num_slots * row_bytes))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "index shares memory with weight");
   sva::CondenseParams p{};
   for (int i = 0; i < n_src; ++i) {
     const int32_t slot = src_slot[i];

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from test_gpu_attend_weights import Case, _chain, _pack
+from test_gpu_condense import _cache
 
 pytestmark = pytest.mark.gpu
 
@@ -56,4 +57,35 @@ def test_weights_out(sva_mod):
     c.cache.attend_weights(c.nodes, out=acc, decay=0.5, **dict(args, prev=acc))
     assert torch.equal(acc, good)
     assert c.cache.poll() == sva_mod.OK
+    c.close()
+
+
+def test_condense_index(sva_mod):
+    """The index over the first and the last bytes of the weights, and next to them on either side."""
+    F, Hp, Wp, H, d, n = 1, 6, 8, 2, 64, 3
+    T = F * Hp * Wp
+    c, src, dst, g = _cache(sva_mod, F, Hp, Wp, H, d, n)
+    w = torch.rand((n + 2, H, T), generator=g, device="cuda")
+    good, good_w = torch.empty((H, T), dtype=torch.int32, device="cuda"), w.clone()
+    c.condense(src, dst, good_w, good)
+    pool = c.slot_pool().view(torch.int16)
+    index_bytes, size = 4 * H * T, 4 * w.numel()
+    for first in (0, 1):
+        for common in (16, 0):
+            buf = torch.zeros(index_bytes + size, dtype=torch.uint8, device="cuda")
+            hi = (size if first else index_bytes) - common
+            weight = _at(buf, 0 if first else hi, w.shape, torch.float32)
+            index = _at(buf, hi if first else 0, (H, T), torch.int32)
+            index.fill_(-5)
+            weight.copy_(w)
+            before, before_pool = buf.clone(), pool.clone()
+            if common:
+                with pytest.raises(sva_mod.SvaError) as e:
+                    c.condense(src, dst, weight, index)
+                assert e.value.status == sva_mod.ERR_INVALID_ARGUMENT
+                torch.cuda.synchronize()
+                assert torch.equal(buf, before) and torch.equal(pool, before_pool)
+            else:
+                c.condense(src, dst, weight, index)
+                assert torch.equal(index, good) and torch.equal(weight, good_w)
     c.close()
