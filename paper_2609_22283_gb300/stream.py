@@ -52,15 +52,20 @@ class Stream:
     def update(self, chunk, level, q, k, v, out, gamma_k=None, gamma_q=None, eps=1e-6):
         """One update of a chunk: q, k, v [1][T][H][d] (dense or parts of a packed projection), out
         [1][T][H][d] receives the attention.  Level 0 is the clean refresh, after which the chunk belongs to
-        the history; other levels leave nothing behind but their share of the weights."""
+        the history; other levels leave nothing behind but their share of the weights.  An update that
+        raises leaves no state behind, so that it can be made again."""
         c = self.cache
         slot = c.bind(0, chunk, level)
-        node = sva.make_nodes([dict(seq=0, chunk=chunk, level=level, own_slot=slot, ctx=self.context())])
-        rotated = torch.empty_like(out)
-        c.rope_kv_write_headnorm(node, k, v, q, rotated, gamma_k, gamma_q, eps)
-        c.attend_nodes(node, rotated, out, self.lse)
-        self.weight[slot].zero_()  # what the slot's last tenant left
-        c.attend_weights(node, rotated, self.lse, self.weight, prev=self.weight, decay=self.decay)
+        try:
+            node = sva.make_nodes([dict(seq=0, chunk=chunk, level=level, own_slot=slot, ctx=self.context())])
+            rotated = torch.empty_like(out)
+            c.rope_kv_write_headnorm(node, k, v, q, rotated, gamma_k, gamma_q, eps)
+            c.attend_nodes(node, rotated, out, self.lse)
+            self.weight[slot].zero_()  # what the slot's last tenant left
+            c.attend_weights(node, rotated, self.lse, self.weight, prev=self.weight, decay=self.decay)
+        except BaseException:
+            c.release(0, chunk, level)
+            raise
         if level != 0:
             c.release(0, chunk, level)
             return
