@@ -374,12 +374,19 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
  *   scale  its logit scale
  *   mask   its masks, or NULL
  *   prev   [num_slots][H][T] fp32, or NULL: nothing before (decay is then not used)
- *   decay  0..1
+ *   decay  0..1, checked without prev too
  *   out    [num_slots][H][T] fp32; only the slots that some node sees are written.
  *          May be prev itself, otherwise shares no memory with it; shares none with
  *          q, lse or a mask
- * fp32 throughout (the products of bf16 accumulate in fp32); the same inputs give
- * the same bits.  Stream-ordered.  Errors: as sva_attend_nodes_masked, plus
+ * A sum belongs to the slot, not to the state bound to it: a slot that was bound anew
+ * goes on from what prev holds for its last state unless the caller sets that to 0.
+ * fp32 throughout (the products of bf16 accumulate in fp32; a single weight below
+ * 2^-126 counts as 0); the same inputs give the same bits.  Launches with token masks
+ * may use the tail of the workspace, as the attention does.  After a device timeout
+ * some sums of out are written and some are not, each one whole: with out = prev the
+ * written ones have this round in them already, so restore or clear them before the
+ * call is made again (two buffers in turn avoid that).
+ * Stream-ordered.  Errors: as sva_attend_nodes_masked, plus
  * INVALID_ARGUMENT for decay or an overlapping out. */
 sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
                               const float* lse, float scale, const sva_attn_mask* mask,
@@ -391,9 +398,11 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
  * the lowest weight.  Their K' and V rows, which carry the positions that they were
  * written at, go to the destination slot in candidate order, their weights to its
  * part of `weight`.  The destination is then a resident state like any other: the
- * attention reads it in one slot where it read n_src.  The sources stay as they are
- * (sva_cache_release frees them; their slots may be written again by later calls on
- * the same stream).
+ * attention reads it in one slot where it read n_src.  Its token v is another token of
+ * the sources in every head (index says which), so the bits of a token mask or tile mask
+ * for it, which are one for all heads, mean nothing there: leave them set.  The sources
+ * stay as they are (sva_cache_release frees them; their slots may be written again by
+ * later calls on the same stream).
  *   src_slot  resident slots, distinct, 1..SVA_MAX_CTX of them
  *   dst_slot  another slot, bound by the caller to a state of the same sequence
  *             whose chunk is not before any source's (so that Eq. 4's causality
@@ -414,8 +423,9 @@ sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_s
  * the device (the softmax of Eq. 4 recombined
  * from per-range maxima and sums), which fills the GPU when a launch has
  * too few work units; results agree with the unsplit computation to
- * rounding.  A long launch of sva_attend_nodes_masked with token masks also
- * keeps there, for its own duration, which key tiles they leave anything of. */
+ * rounding.  A long launch of sva_attend_nodes_masked or sva_attend_weights
+ * with token masks also keeps there, for its own duration, which key tiles they
+ * leave anything of. */
 size_t sva_attend_workspace_bytes(const sva_cache* c);
 
 /* Attaches a caller-owned device buffer of at least

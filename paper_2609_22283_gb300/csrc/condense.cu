@@ -444,8 +444,9 @@ cudaError_t launch_condense(CondenseParams& p, int num_sms, cudaStream_t s) {
     }
   }
   const int n = p.n_src * p.T;
-  // About 2048 candidates a CTA, at most eight CTAs a head, and no more of them than
-  // run at once (two an SM).
+  // About 2048 candidates a CTA, at most eight CTAs a head, and no more of them than two
+  // an SM.  (A CTA with more than about 14000 candidates has an SM to itself: where there
+  // are more such CTAs than SMs, the last ones run after others.)
   int log2_cluster = 0;
   while (log2_cluster < 3 && n > 2048 << log2_cluster && (long long)p.H << (log2_cluster + 1) <= 2ll * num_sms)
     ++log2_cluster;

@@ -1411,7 +1411,8 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
   const long long units = (long long)n_slots * g.num_heads * p.n_pairs;  // < 2^23: the pool has < 2^31 rows
   p.units = (int32_t)units;
   // A unit whose SMs would otherwise idle is shared by a cluster, two Q tiles a
-  // CTA at least.
+  // CTA at least.  (How many such clusters fit at once is not asked: where that is
+  // fewer, the last ones run after others.)
   const long long tiles = (long long)fewest * p.n_qt;
   p.n_split = (int32_t)std::max(1ll, std::min({(long long)sva::kMaxWeightSplit, c->num_sms / units, tiles / 2}));
   long long grid = units * p.n_split;

@@ -28,8 +28,8 @@ CONDENSED = 1 << 20  # the level under which a condensed state is bound
 class Stream:
     def __init__(self, H, d, F, Hp, Wp, pairs, max_frames, window=6, recent=3, decay=1.0, theta=10000.0,
                  device="cuda"):
-        """window: clean states kept whole; recent: how many of them stay whole when the older ones are
-        condensed (1..window); decay: of the weights from update to update, 0..1."""
+        """window: clean states kept whole, up to MAX_CTX - 2; recent: how many of them stay whole when the
+        older ones are condensed (1..window); decay: of the weights from update to update, 0..1."""
         if not 1 <= recent <= window or window + 2 > sva.MAX_CTX:
             raise ValueError(f"need 1 <= recent <= window <= {sva.MAX_CTX - 2}")
         g = sva.make_geometry(H, d, F, Hp, Wp, num_slots=window + 3, pairs=pairs, max_frames=max_frames,
