@@ -73,6 +73,7 @@ enum {
 
 #define SVA_MAX_CTX 16   /* history states one node may read */
 #define SVA_MAX_NODES 64 /* nodes in one sva_rope_kv_write / sva_attend_nodes call */
+#define SVA_PACKED (1 << 30) /* slot numbers from here on name packed slots (sva_cache_set_packed) */
 
 typedef struct sva_cache sva_cache;
 typedef struct CUstream_st* sva_stream; /* a cudaStream_t; NULL = legacy default stream */
@@ -415,6 +416,79 @@ sva_status sva_attend_weights(sva_cache* c, const sva_node* nodes, int32_t n_nod
  * CUDA. */
 sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_src, int32_t dst_slot,
                               float* weight, int32_t* index, sva_stream s);
+
+/* ---- States in 4 bits ----
+ *
+ * Old states of a long history may be held in packed slots, in 0.28 of a slot's bytes.
+ * Each 32 neighbouring elements of one token's K' or V row of a head have a scale s,
+ * their largest magnitude a divided by 7 and rounded to 5 significant bits (halves up),
+ * and each element x is held as the whole number nearest to x / s (halves away from
+ * zero), -7 to 7.  It stands for that number times s, which is a bf16 number, so that
+ * reading back rounds nothing, and packing what was read back gives the same again.  An
+ * element is off by at most s / 2, about a / 14.  A group with a < 2^-120 holds zeros;
+ * one with a NaN, an infinity or a >= 2^124 reads as NaN throughout.
+ *
+ * Packed slots are numbered from SVA_PACKED on and have a table of their own beside that of
+ * the slots: a state may be in a slot, in a packed slot, or in both.  They stand in a node's
+ * ctx_slot for sva_attend_nodes_packed, and for no other call but those below. */
+
+/* Bytes of device memory of `num_packed` (1..2^20) packed slots: per slot [2 (K, V)][H]
+ * tiles of 128 tokens, each d / 2 bytes of numbers and d / 16 bytes of scales a token.  0
+ * if `g` or num_packed is invalid. */
+size_t sva_packed_bytes(const sva_geometry* g, int32_t num_packed);
+
+/* Attaches the caller's buffer of at least sva_packed_bytes(g, num_packed) bytes (256-byte
+ * aligned, on the cache's device, no memory of the cache's buffer or workspace) as
+ * the cache's packed slots, or detaches them when dev_buf is NULL.  No packed slot may be bound.
+ * The buffer must outlive its use.  Host-side only.  Errors: INVALID_ARGUMENT. */
+sva_status sva_cache_set_packed(sva_cache* c, void* dev_buf, size_t bytes, int32_t num_packed);
+
+/* sva_cache_bind, _lookup and _release for packed slots.  The number is SVA_PACKED or more.
+ * Errors: as those. */
+sva_status sva_cache_bind_packed(sva_cache* c, int32_t seq, int32_t chunk, int32_t level, int32_t* slot);
+sva_status sva_cache_lookup_packed(const sva_cache* c, int32_t seq, int32_t chunk, int32_t level, int32_t* slot);
+sva_status sva_cache_release_packed(sva_cache* c, int32_t seq, int32_t chunk, int32_t level);
+
+/* Puts the states of n slots into n packed slots, in one launch: state i from slot[i] to
+ * packed[i].  The slots stay as they are (sva_cache_release frees them; their slots may be
+ * written again by later calls on the same stream).  Marks the packed slots resident.
+ *   slot     resident slots; one may be given several times
+ *   packed   distinct packed slots, each bound by the caller to a state of the same sequence
+ *            whose chunk is not before the source's (so that Eq. 4's causality holds
+ *            for what it contains): usually the same state
+ *   n        1..SVA_MAX_NODES
+ * Stream-ordered.  Errors: INVALID_ARGUMENT, NOT_RESIDENT (a source), CAUSALITY (another
+ * sequence, or an earlier chunk than the source's), CAPACITY (n), CUDA. */
+sva_status sva_cache_pack(sva_cache* c, const int32_t* slot, const int32_t* packed, int32_t n, sva_stream s);
+
+/* The way back: reads packed[i] into slot[i], which then is a resident slot with the values
+ * that the 4 bits stand for.  Packed slots may be given several times, slots are distinct;
+ * conditions and errors otherwise as sva_cache_pack. */
+sva_status sva_cache_unpack(sva_cache* c, const int32_t* packed, const int32_t* slot, int32_t n, sva_stream s);
+
+/* sva_attend_nodes_masked where contexts may be packed slots (own slots are not).  The
+ * attention is that over the values which the packed slots stand for: the keys and values are
+ * the same as after sva_cache_unpack.  Everything else, masks included, as for
+ * sva_attend_nodes_masked; `mask` may be NULL.  A launch without a visible packed context gives
+ * the bits of sva_attend_nodes_masked.  Errors: as sva_attend_nodes_masked. */
+sva_status sva_attend_nodes_packed(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
+                                   void* out, float* lse, float scale, const sva_attn_mask* mask,
+                                   sva_stream s);
+
+/* Copies n states in one launch: from src_slot[i] of `from` to dst_slot[i] of `to`, which may
+ * be the same cache (a video branches: the states of its sequence copied to those of a new one) or
+ * another one on the same device (a cache is grown or compacted).  The slots of a call are all packed ones,
+ * or none is.  Rows keep the positions that they were written at.  Marks the destinations resident.
+ *   src_slot  resident slots; one may be given several times
+ *   dst_slot  distinct slots, bound by the caller to states of any sequence whose chunk is not
+ *             before the source's; none of them a source of the same call
+ *   n         1..SVA_MAX_NODES
+ * The caches agree in everything that a state's rows depend on: heads, head dimension, frames,
+ * grid, rope_pairs, rope_theta.  Stream-ordered (both caches' calls on the one stream).  Errors:
+ * INVALID_ARGUMENT, NOT_RESIDENT (a source), CAUSALITY (an earlier chunk than the source's),
+ * CAPACITY (n), CUDA. */
+sva_status sva_cache_copy(sva_cache* from, const int32_t* src_slot, sva_cache* to, const int32_t* dst_slot,
+                          int32_t n, sva_stream s);
 
 /* Bytes of the optional split workspace of a cache (0 if c is NULL).  With
  * a workspace attached, sva_attend_nodes may divide each (node, head,

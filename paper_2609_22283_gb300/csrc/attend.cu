@@ -22,14 +22,18 @@ cudaError_t configure_d(int dev) {
   for (AttendKernel k :
        {attend_dense_kernel(D), attend_masked_kernel(D, false), attend_masked_kernel(D, true),
         attend_cluster_kernel(D, false, false), attend_cluster_kernel(D, true, false),
-        attend_cluster_kernel(D, true, true)}) {
+        attend_cluster_kernel(D, true, true), attend_packed_kernel(D, false, false),
+        attend_packed_kernel(D, false, true), attend_packed_kernel(D, true, false),
+        attend_packed_kernel(D, true, true)}) {
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          AttnCfg<D>::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaFuncAttributes fa;
     e = cudaFuncGetAttributes(&fa, k);
     if (e != cudaSuccess) return e;
-    if (fa.numRegs * kThreads < AttnRegs<D>::kPool) return cudaErrorInvalidConfiguration;
+    const bool packed = fa.maxThreadsPerBlock == kPackedThreads;
+    const int pool = packed ? AttnRegs<D, true>::kPool : AttnRegs<D>::kPool;
+    if (fa.numRegs * (packed ? kPackedThreads : kThreads) < pool) return cudaErrorInvalidConfiguration;
   }
   configured[dev] = true;
   return cudaSuccess;
@@ -43,11 +47,13 @@ cudaError_t launch_d(const AttnParams& p, int grid, cudaStream_t s) {
   e = configure_d<D>(dev);
   if (e != cudaSuccess) return e;
   const bool token = p.masked && (p.own_mask != nullptr || p.hist_mask != nullptr);
-  LaunchConfig l(dim3((unsigned)grid), kThreads, AttnCfg<D>::kSmemBytes, s,
+  const bool packed = p.packed != nullptr;
+  LaunchConfig l(dim3((unsigned)grid), packed ? kPackedThreads : kThreads, AttnCfg<D>::kSmemBytes, s,
                  p.cluster ? p.n_split : 0);
-  AttendKernel k = p.cluster  ? attend_cluster_kernel(D, p.masked, token)
-                   : p.masked ? attend_masked_kernel(D, token)
-                              : attend_dense_kernel(D);
+  AttendKernel k = packed      ? attend_packed_kernel(D, p.masked, p.cluster)
+                   : p.cluster ? attend_cluster_kernel(D, p.masked, token)
+                   : p.masked  ? attend_masked_kernel(D, token)
+                               : attend_dense_kernel(D);
   return cudaLaunchKernelEx(&l.cfg, k, p);
 }
 

@@ -70,6 +70,7 @@
 #include <cuda_runtime.h>
 
 #include "internal.h"
+#include "packed.cuh"
 #include "ptx.cuh"
 
 namespace sva {
@@ -121,14 +122,20 @@ __device__ __forceinline__ uint32_t col_o(int b) {
 // kRegsHigh).  The split must fit the launch's pool: 4*32*kRegsLow +
 // 8*32*kRegsHigh <= 384*kLaunchRegs, checked at launch.  At D = 64 a softmax
 // thread holds 128 scores and spills below 216 (88 + 208 was 3% slower).
+//
+// Instances that read packed slots have a fourth warpgroup (warps 12-15), which
+// turns packed tiles into bf16 ones; 512 threads are launched with 128 registers
+// each, and the warpgroups other than the softmax's keep kLow.
 constexpr int kThreads = 384;
-constexpr int kLaunchRegs = 168;
-template <int D>
+constexpr int kPackedThreads = 512;
+template <int D, bool kPacked = false>
 struct AttnRegs {
-  static constexpr int kLow = D == 128 ? 88 : 72;
-  static constexpr int kHigh = D == 128 ? 208 : 216;
-  static constexpr int kPool = 4 * 32 * kLow + 8 * 32 * kHigh;
-  static_assert(kPool <= kThreads * kLaunchRegs, "register split");
+  static constexpr int kThreadsOf = kPacked ? kPackedThreads : kThreads;
+  static constexpr int kLaunch = kPacked ? 128 : 168;
+  static constexpr int kLow = kPacked ? (D == 128 ? 56 : 40) : (D == 128 ? 88 : 72);
+  static constexpr int kHigh = kPacked ? (D == 128 ? 200 : 216) : (D == 128 ? 208 : 216);
+  static constexpr int kPool = (kThreadsOf - 256) * kLow + 256 * kHigh;
+  static_assert(kPool <= kThreadsOf * kLaunch, "register split");
 };
 // Lazy rescale of O: a row's running max m is only moved (and O, l scaled)
 // when a tile's max exceeds it by more than this many log2 units, so P =
@@ -207,6 +214,15 @@ struct Bars {
   uint64_t v_full[6];
   uint64_t v_empty[6];
 };
+
+// Packed tiles (kPacked): the producer says that stage s may be filled, the unpacking
+// warps wait for it.  They are the only ones that wait, and wait for every phase; a
+// stage's next phase needs the tile that they put there.
+struct PackBars {
+  uint64_t k_go[4];
+  uint64_t v_go[6];
+};
+constexpr int kUnpackWarps = 4;
 
 // Block-sparse launches: a role's walk over the key tiles that either query
 // tile of the unit may attend (bitmaps in the kernel's tile order).  The
@@ -313,13 +329,16 @@ __device__ __forceinline__ void record_timeout(const AttnParams& p, volatile int
 // split over the CTAs of one cluster, which merge through their shared memory.
 // Each extra feature costs the per-tile loop, so a launch takes the leanest
 // instance that covers it.
-template <int D, bool kSparse, bool kToken, bool kCluster>
-__global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_constant__ AttnParams p) {
+template <int D, bool kSparse, bool kToken, bool kCluster, bool kPacked = false>
+__global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
+    attend_kernel(const __grid_constant__ AttnParams p) {
   using C = AttnCfg<D>;
+  using R = AttnRegs<D, kPacked>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   __shared__ Bars bars;
+  __shared__ PackBars pack;  // kPacked
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
   __shared__ int last_split;
@@ -384,6 +403,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   uint8_t* sQ1 = smem + C::kOffQ1;
   uint8_t* sK = smem + C::kOffK;
   uint8_t* sV = smem + C::kOffV;
+  // A copy into a K or V stage: all the arrivals that its barrier counts, one of them
+  // with the bytes.
+  auto expect_tile = [&](uint64_t* bar) {
+    mbar_arrive_expect_tx(bar, C::kTileBytes);
+    if constexpr (kPacked)
+      for (int w = 1; w < kUnpackWarps; ++w) mbar_arrive(bar);
+  };
+  auto is_packed = [](int slot) { return kPacked && slot >= kPackedSlot; };
   auto load_q = [&]() {
     mbar_arrive_expect_tx(&bars.q_full, (has_q1 ? 2 : 1) * C::kTileBytes);
 #pragma unroll
@@ -407,11 +434,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       mbar_init(&bars.p_full[b], 128 * C::kRowThreads);
     }
     for (int s = 0; s < C::kKStages; ++s) {
-      mbar_init(&bars.k_full[s], 1);
+      mbar_init(&bars.k_full[s], kPacked ? kUnpackWarps : 1);
+      if constexpr (kPacked) mbar_init(&pack.k_go[s], 1);
       mbar_init(&bars.k_empty[s], C::kOwnTile && has_q1 ? 2 : 1);  // D = 64: one per query tile
     }
     for (int s = 0; s < C::kVStages; ++s) {
-      mbar_init(&bars.v_full[s], 1);
+      mbar_init(&bars.v_full[s], kPacked ? kUnpackWarps : 1);
+      if constexpr (kPacked) mbar_init(&pack.v_go[s], 1);
       mbar_init(&bars.v_empty[s], C::kOwnTile && has_q1 ? 2 : 1);
     }
     fence_mbar_init();
@@ -423,12 +452,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       load_q();
       if (n_tiles > 0) {
         const int st = t_begin / p.nt_slot;
-        const int row_k = (nd.slot[st] * 2 * p.H + h) * p.Tpad + (t_begin - st * p.nt_slot) * kTile;
-        const uint64_t keep = l2_policy_evict_last();
-        mbar_arrive_expect_tx(&bars.k_full[0], C::kTileBytes);
+        if (is_packed(nd.slot[st])) {
+          if constexpr (kPacked) mbar_arrive(&pack.k_go[0]);
+        } else {
+          const int row_k = (nd.slot[st] * 2 * p.H + h) * p.Tpad + (t_begin - st * p.nt_slot) * kTile;
+          const uint64_t keep = l2_policy_evict_last();
+          expect_tile(&bars.k_full[0]);
 #pragma unroll
-        for (int b = 0; b < C::kBoxes; ++b)
-          tma_load_2d_hint(sK + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full[0], b * 64, row_k, keep);
+          for (int b = 0; b < C::kBoxes; ++b)
+            tma_load_2d_hint(sK + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full[0], b * 64, row_k, keep);
+        }
       }
     }
   }
@@ -500,9 +533,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   const uint64_t tmo = p.timeout_ns;
 
   int k_issued = 0, v_issued = 0;  // producer: tiles whose K / V copies were started
+  uint32_t k_copy = 0, v_copy = 0;  // kPacked: stages whose last tile is a copy
 
   if (warp < 4) {
-    regs_dec<AttnRegs<D>::kLow>();
+    regs_dec<R::kLow>();
     if (warp == 0) {
     // ------------------------------------------------------------ producer
     if (lane == 0) {
@@ -514,7 +548,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       for (int j = 0; j < n_tiles; ++j, i = sparse ? walk.next() : next_kt(i)) {
         const int ks = j % C::kKStages;
         const int vs = j % C::kVStages;
-        const int slot = nd.slot[i / p.nt_slot];
+        const bool packed = is_packed(nd.slot[i / p.nt_slot]);
+        const int slot = packed ? 0 : nd.slot[i / p.nt_slot];  // (no row of a packed one is worked out)
         const int t = i - (i / p.nt_slot) * p.nt_slot;
         const int row_k = ((slot * 2 + 0) * p.H + h) * p.Tpad + t * kTile;
         const int row_v = row_k + p.H * p.Tpad;
@@ -524,12 +559,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
             record_timeout(p, &abort_flag);
             break;
           }
-          mbar_arrive_expect_tx(&bars.k_full[ks], C::kTileBytes);
+          if (packed) {
+            if constexpr (kPacked) mbar_arrive(&pack.k_go[ks]);
+          } else {
+            expect_tile(&bars.k_full[ks]);
 #pragma unroll
-          for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_2d_hint(sK + ks * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
-                             &bars.k_full[ks], b * 64, row_k, keep);
+            for (int b = 0; b < C::kBoxes; ++b)
+              tma_load_2d_hint(sK + ks * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
+                               &bars.k_full[ks], b * 64, row_k, keep);
+          }
         }
+        if constexpr (kPacked) k_copy = packed ? k_copy & ~(1u << ks) : k_copy | 1u << ks;
         k_issued = j + 1;
         if (!mbar_wait(&bars.v_empty[vs], ((uint32_t)(j / C::kVStages) & 1u) ^ 1u, &abort_flag,
                        tmo)) {
@@ -538,12 +578,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
         }
         // fault_mode 1 (test hook): withhold the V copy of the second tile,
         // so the MMA issuer's bounded wait on it expires.
+        if constexpr (kPacked) v_copy = packed ? v_copy & ~(1u << vs) : v_copy | 1u << vs;
         if (!(p.fault_mode == 1 && j == 1)) {
-          mbar_arrive_expect_tx(&bars.v_full[vs], C::kTileBytes);
+          if (packed) {
+            if constexpr (kPacked) mbar_arrive(&pack.v_go[vs]);
+          } else {
+            expect_tile(&bars.v_full[vs]);
 #pragma unroll
-          for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_2d_hint(sV + vs * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
-                             &bars.v_full[vs], b * 64, row_v, keep);
+            for (int b = 0; b < C::kBoxes; ++b)
+              tma_load_2d_hint(sV + vs * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
+                               &bars.v_full[vs], b * 64, row_v, keep);
+          }
         }
         v_issued = j + 1;
       }
@@ -731,10 +776,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       const int zero = 0;
       if (warp == 0 && lane == 0) {
         mbar_wait(&bars.q_full, 0, &zero, tmo);
-        for (int i = (k_issued > C::kKStages ? k_issued - C::kKStages : 0); i < k_issued; ++i)
+        for (int i = (k_issued > C::kKStages ? k_issued - C::kKStages : 0); i < k_issued; ++i) {
+          if (kPacked && !((k_copy >> (i % C::kKStages)) & 1u)) continue;  // no copy
           mbar_wait(&bars.k_full[i % C::kKStages], (uint32_t)(i / C::kKStages) & 1u, &zero, tmo);
+        }
         for (int i = (v_issued > C::kVStages ? v_issued - C::kVStages : 0); i < v_issued; ++i) {
           if (p.fault_mode == 1 && i == 1) continue;  // the copy the test hook withheld
+          if (kPacked && !((v_copy >> (i % C::kVStages)) & 1u)) continue;
           mbar_wait(&bars.v_full[i % C::kVStages], (uint32_t)(i / C::kVStages) & 1u, &zero, tmo);
         }
       } else if (warp == 1 || warp == 3) {
@@ -747,8 +795,89 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       tc_fence_after();
       tmem_dealloc(tbase, C::kTmemCols);
     }
+  } else if (kPacked && warp >= 12) {
+    regs_dec<R::kLow>();
+    // ------------------------------------------------------------ unpacking
+    // Each warp fills 32 rows of a tile, a thread one: its 4-bit words are loaded a tile
+    // (K or V) ahead, each vector into the registers that the one in front of it has just
+    // left, and go to the stage as the bf16 values that they stand for, in the layout in
+    // which a copy would have put them there.
+    if constexpr (kPacked) {
+      constexpr int G = D / kPackGroup;  // vectors of 32 elements in a row
+      const int r = (int)threadIdx.x - 384;
+      const uint32_t row_off = (uint32_t)r * 128u, turn = (uint32_t)(r & 7);
+      const size_t v_off = (size_t)p.H * p.nt_slot * kPackTileBytes<D>;  // from K to V of a state
+      TileWalk<kSparse ? kMaskWords : 1> walk;
+      if constexpr (sparse) walk.start(tmask, t_begin, n_all);
+      int kt = sparse ? walk.next() : t_begin, j = 0;
+      // To the next packed tile at or after the walk's place: its K of this head, or null.
+      auto seek = [&]() -> const uint8_t* {
+        for (; j < n_tiles; ++j, kt = sparse ? walk.next() : next_kt(kt)) {
+          const int st = kt / p.nt_slot;
+          const int slot = nd.slot[st];
+          if (is_packed(slot))
+            return p.packed + (((size_t)(slot - kPackedSlot) * 2 * p.H + h) * p.nt_slot + (kt - st * p.nt_slot)) *
+                                  kPackTileBytes<D>;
+        }
+        return nullptr;
+      };
+      const uint8_t* at = seek();
+      PackRow<D> row;
+      if (at != nullptr) row.load_all(at, r);
+      uint32_t k_par = 0, v_par = 0;  // phase of each stage's go barrier
+      bool ok = true;
+      while (ok && at != nullptr) {
+        const int tile = j;
+        const uint8_t* v_at = at + v_off;
+        ++j;
+        kt = sparse ? walk.next() : next_kt(kt);
+        const uint8_t* next = seek();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int stages = half ? C::kVStages : C::kKStages;
+          const int s = tile % stages;
+          uint32_t& par = half ? v_par : k_par;
+          ok = mbar_wait(half ? &pack.v_go[s] : &pack.k_go[s], (par >> s) & 1u, &abort_flag, tmo);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          par ^= 1u << s;
+          const uint32_t dst = smem_u32(half ? sV : sK) + (uint32_t)s * C::kTileBytes + row_off;
+          // (the last tile loads itself again: in bounds, and not used)
+          const uint8_t* then = half ? (next != nullptr ? next : v_at) : v_at;
+          const typename PackRow<D>::Scales scales = row.scales;
+          row.load_scales(then, r);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint32_t sc = PackRow<D>::scale(scales, g);
+            const uint4 c = row.codes[g];
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int cc = g * 4 + k;  // 16-byte piece of the row
+              const uint4 x = packed_values(w[k], sc);
+              st_shared_v4(dst + (uint32_t)((cc >> 3) * C::kBoxBytes) + ((((uint32_t)cc & 7u) ^ turn) << 4), x.x, x.y,
+                           x.z, x.w);
+            }
+            row.load_codes(then, r, g);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(half ? &bars.v_full[s] : &bars.k_full[s]);
+        }
+        at = next;
+      }
+      if (!ok && lane == 0) record_timeout(p, &abort_flag);
+    }
+    // ---------------------------------------------------------------- teardown (unpacking)
+    __syncwarp();
+    if constexpr (kCluster) {  // the two barriers of the merge
+      cluster_sync();
+      cluster_sync();
+    }
+    tc_fence_before();
+    __syncthreads();
   } else {
-    regs_inc<AttnRegs<D>::kHigh>();
+    regs_inc<R::kHigh>();
     // ------------------------------------------------------------ softmax + epilogue
     // D = 128: all eight softmax warps work on one query tile at a time (tile
     // 0, then tile 1, of every key tile).  A warp covers 16 rows, half of its
@@ -1477,5 +1606,7 @@ AttendKernel attend_dense_kernel(int head_dim);
 AttendKernel attend_masked_kernel(int head_dim, bool token);
 // Each unit split over a cluster.
 AttendKernel attend_cluster_kernel(int head_dim, bool masked, bool token);
+// Nodes that read packed slots.
+AttendKernel attend_packed_kernel(int head_dim, bool masked, bool cluster);
 
 }  // namespace sva

@@ -1,0 +1,50 @@
+// Packed slots: states in 4 bits, their layout, and the launch parameters of the
+// kernels that fill and read them (packed.cu) and that copy states (state_copy.cu).
+//
+// A packed slot is [2 (K, V)][H][tiles of 128 tokens], a tile's bytes
+//   codes   [d / 32][128 tokens][16]: the 32 codes of a token's group g of elements
+//   scales  [128 tokens][d / 32] bf16
+// so that the threads that take a tile's tokens one each read whole lines, and a
+// tile is one piece of memory.  Tokens past T have scale 0.
+//
+// Byte order of a group: 32-bit word k holds elements 8k..8k+7; element 8k + 2j has
+// the four bits from 4j on, element 8k + 2j + 1 those from 16 + 4j on, each as its
+// code + 8 (1..15).  So a shift and a mask leave two neighbouring elements in the two
+// halves of a word (packed_values in packed.cuh).
+#pragma once
+
+#include "internal.h"
+
+namespace sva {
+
+constexpr int kPackGroup = 32;  // elements that share a scale
+
+constexpr int pack_tile_bytes(int d) { return kTile * (d / 2 + d / kPackGroup * 2); }
+template <int D>
+constexpr int kPackTileBytes = pack_tile_bytes(D);
+
+struct PackParams {
+  void* pool;       // slot pool base, bf16 [num_slots][2][H][Tpad][d]
+  uint8_t* packed;  // packed slots
+  int32_t T, Tpad, H;
+  int32_t n;
+  int32_t slot[SVA_MAX_NODES];    // state i: its slot
+  int32_t number[SVA_MAX_NODES];  // and its packed slot, from 0
+};
+
+// Slots to packed slots, and back (d = 64 or 128).
+cudaError_t launch_pack(const PackParams& p, int d, cudaStream_t s);
+cudaError_t launch_unpack(const PackParams& p, int d, cudaStream_t s);
+
+struct StateCopyParams {
+  uint32_t plane;        // 32-byte vectors of a plane that are copied
+  uint32_t vectors;      // of a state: all its planes'
+  int64_t plane_stride;  // bytes
+  int32_t n;
+  const uint8_t* src[SVA_MAX_NODES];
+  uint8_t* dst[SVA_MAX_NODES];
+};
+
+cudaError_t launch_state_copy(const StateCopyParams& p, cudaStream_t s);
+
+}  // namespace sva

@@ -22,6 +22,7 @@
 
 #include "condense.h"
 #include "internal.h"
+#include "packed.h"
 #include "proj.h"
 #include "rope_head.h"
 #include "sva.h"
@@ -166,6 +167,8 @@ struct SlotInfo {
 
 using StateKey = std::tuple<int32_t, int32_t, int32_t>;
 
+constexpr int32_t kMaxPacked = 1 << 20;  // packed slots of a cache
+
 // (cos, sin) of pos * theta^(-i / pairs) for pos in [0, npos), i in [0, pairs),
 // evaluated in fp64 and rounded once to fp32.
 std::vector<float2> rope_table(int npos, int pairs, double theta) {
@@ -239,9 +242,27 @@ struct sva_cache {
   int fault_mode = 0;  // one-shot test hook, see sva_debug_inject
   uint64_t timeout_ns = sva::kDefaultWaitTimeoutNs;
   char* ws = nullptr;  // caller's split workspace (sva_cache_set_workspace), or null
+  uint8_t* packed = nullptr;  // caller's packed slots (sva_cache_set_packed), or null
+  std::vector<SlotInfo> packed_slots;
+  std::map<StateKey, int32_t> packed_index;  // values, and the stack: from 0, without SVA_PACKED
+  std::vector<int32_t> packed_free;
 };
 
 namespace {
+
+// Bytes of one packed slot.
+size_t packed_slot_bytes(const sva_geometry& g, const Layout& L) {
+  return (size_t)2 * g.num_heads * (L.Tpad / sva::kTile) * sva::pack_tile_bytes(g.head_dim);
+}
+
+// The table's entry of a slot, packed or not; null for a number that is neither.
+SlotInfo* slot_info(sva_cache* c, int32_t slot) {
+  if (slot >= 0 && slot < c->g.num_slots) return &c->slots[slot];
+  if (slot >= SVA_PACKED && (size_t)(slot - SVA_PACKED) < c->packed_slots.size())
+    return &c->packed_slots[slot - SVA_PACKED];
+  return nullptr;
+}
+const SlotInfo* slot_info(const sva_cache* c, int32_t slot) { return slot_info(const_cast<sva_cache*>(c), slot); }
 
 sva_status check_device(const sva_cache* c) {
   int dev = -1;
@@ -292,8 +313,12 @@ sva_status check_written(const sva_cache* c, const sva_node* nodes, int n_nodes,
 
 // The checks of the states that nodes read, and each node's list of the slots
 // it sees (own first, then the visible contexts).
-sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sva::AttnNode* out) {
+// packed: where not NULL contexts may be packed slots, and *packed says whether a
+// visible one is.
+sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sva::AttnNode* out,
+                      bool* packed = nullptr) {
   const sva_geometry& g = c->g;
+  if (packed != nullptr) *packed = false;
   for (int i = 0; i < n_nodes; ++i) {
     const sva_node& n = nodes[i];
     sva_status st = check_own(c, n, i, true);
@@ -310,9 +335,11 @@ sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sv
     int nkv = 1;
     for (int k = 0; k < n.n_ctx; ++k) {
       const int32_t cs = n.ctx_slot[k];
-      if (cs < 0 || cs >= g.num_slots)
-        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d: slot %d out of range", i, k, cs);
-      const SlotInfo& si = c->slots[cs];
+      const SlotInfo* known = slot_info(c, cs);
+      if (known == nullptr || (packed == nullptr && cs >= g.num_slots))
+        return fail(SVA_ERR_INVALID_ARGUMENT, "node %d ctx %d: slot %d out of range%s", i, k, cs,
+                    cs >= SVA_PACKED && packed == nullptr ? " (a packed slot, which sva_attend_nodes_packed reads)" : "");
+      const SlotInfo& si = *known;
       if (!si.bound || !si.resident)
         return fail(SVA_ERR_NOT_RESIDENT, "node %d ctx %d: slot %d is %s", i, k, cs,
                     si.bound ? "bound but not written" : "not bound");
@@ -329,6 +356,7 @@ sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sv
       if (n.ctx_visible[k]) {
         a.src[nkv] = (uint8_t)(1 + k);
         a.slot[nkv++] = cs;
+        if (cs >= SVA_PACKED) *packed = true;
       }
     }
     a.n_kv = nkv;
@@ -687,6 +715,84 @@ sva_status sva_cache_release(sva_cache* c, int32_t seq, int32_t chunk, int32_t l
   return ok();
 }
 
+size_t sva_packed_bytes(const sva_geometry* g, int32_t num_packed) {
+  sva_status st;
+  if (!geometry_valid(g, &st)) return 0;
+  if (num_packed < 1 || num_packed > kMaxPacked) {
+    fail(SVA_ERR_INVALID_ARGUMENT, "num_packed %d outside 1..%d", num_packed, kMaxPacked);
+    return 0;
+  }
+  return (size_t)num_packed * packed_slot_bytes(*g, layout_of(*g));
+}
+
+sva_status sva_cache_set_packed(sva_cache* c, void* dev_buf, size_t bytes, int32_t num_packed) {
+  if (c == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL cache");
+  if (!c->packed_index.empty())
+    return fail(SVA_ERR_INVALID_ARGUMENT, "%zu packed slots are bound: release them first", c->packed_index.size());
+  if (dev_buf != nullptr) {
+    const size_t need = sva_packed_bytes(&c->g, num_packed);
+    if (need == 0) return SVA_ERR_INVALID_ARGUMENT;
+    if ((reinterpret_cast<uintptr_t>(dev_buf) & 255u) != 0)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "packed slots must be 256-byte aligned");
+    if (bytes < need)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "buffer of %zu bytes is smaller than the %zu needed", bytes, need);
+    if (!on_device(dev_buf, c->device))
+      return fail(SVA_ERR_INVALID_ARGUMENT, "packed slots are not device memory of the cache's device");
+    if (share_memory(dev_buf, need, c->base, c->L.total) ||
+        share_memory(dev_buf, need, c->ws, c->ws != nullptr ? ws_total_bytes(c) : 0))
+      return fail(SVA_ERR_INVALID_ARGUMENT, "packed slots share memory with the cache's buffer or its workspace");
+  }
+  c->packed = static_cast<uint8_t*>(dev_buf);
+  c->packed_slots.assign(dev_buf != nullptr ? num_packed : 0, SlotInfo());
+  c->packed_free.clear();
+  for (int32_t s = (int32_t)c->packed_slots.size() - 1; s >= 0; --s) c->packed_free.push_back(s);
+  return ok();
+}
+
+sva_status sva_cache_bind_packed(sva_cache* c, int32_t seq, int32_t chunk, int32_t level, int32_t* slot) {
+  if (c == nullptr || slot == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  if (level < 0) return fail(SVA_ERR_INVALID_ARGUMENT, "level %d < 0", level);
+  const StateKey k{seq, chunk, level};
+  auto it = c->packed_index.find(k);
+  if (it != c->packed_index.end())
+    return fail(SVA_ERR_INVALID_ARGUMENT, "(seq %d, chunk %d, level %d) is already bound to packed slot %d", seq,
+                chunk, level, SVA_PACKED + it->second);
+  if (c->packed_free.empty())
+    return fail(SVA_ERR_CAPACITY, "all %zu packed slots are bound", c->packed_slots.size());
+  const int32_t s = c->packed_free.back();
+  c->packed_free.pop_back();
+  SlotInfo& si = c->packed_slots[s];
+  si.bound = true;
+  si.resident = false;
+  si.seq = seq;
+  si.chunk = chunk;
+  si.level = level;
+  c->packed_index[k] = s;
+  *slot = SVA_PACKED + s;
+  return ok();
+}
+
+sva_status sva_cache_lookup_packed(const sva_cache* c, int32_t seq, int32_t chunk, int32_t level, int32_t* slot) {
+  if (c == nullptr || slot == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  auto it = c->packed_index.find(StateKey{seq, chunk, level});
+  if (it == c->packed_index.end())
+    return fail(SVA_ERR_NOT_RESIDENT, "(seq %d, chunk %d, level %d) is not in a packed slot", seq, chunk, level);
+  *slot = SVA_PACKED + it->second;
+  return ok();
+}
+
+sva_status sva_cache_release_packed(sva_cache* c, int32_t seq, int32_t chunk, int32_t level) {
+  if (c == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  auto it = c->packed_index.find(StateKey{seq, chunk, level});
+  if (it == c->packed_index.end())
+    return fail(SVA_ERR_NOT_RESIDENT, "(seq %d, chunk %d, level %d) is not in a packed slot", seq, chunk, level);
+  const int32_t s = it->second;
+  c->packed_index.erase(it);
+  c->packed_slots[s] = SlotInfo();
+  c->packed_free.push_back(s);
+  return ok();
+}
+
 sva_status sva_select_context(int32_t policy, int32_t K, int32_t W, int32_t chunk, int32_t level,
                               int32_t cap, int32_t* chunks, int32_t* levels, int32_t* n) {
   if (chunks == nullptr || levels == nullptr || n == nullptr)
@@ -923,11 +1029,13 @@ enum class Scratch {
   kStatic,     // the library's static device array (sva_attend_nodes_noalloc)
 };
 
-// sva_attend_nodes, _sparse, _masked and _noalloc: the checks, the launch
-// parameters, the split plan and the launch.  A mask of NULLs is the dense mask.
+// sva_attend_nodes, _sparse, _masked, _packed (packed_slots: contexts may be packed
+// slots) and _noalloc: the checks, the launch parameters, the split plan and the
+// launch.  A mask of NULLs is the dense mask.
 // Every check runs before anything is enqueued.
 sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q, void* out,
-                  float* lse, float scale, const sva_attn_mask& mask, sva_stream s, Scratch scratch) {
+                  float* lse, float scale, const sva_attn_mask& mask, sva_stream s, Scratch scratch,
+                  bool packed_slots = false) {
   if (c == nullptr || nodes == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
   if (n_nodes < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_nodes %d < 1", n_nodes);
   if (n_nodes > SVA_MAX_NODES)
@@ -943,8 +1051,10 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
 
   static thread_local sva::AttnParams p;  // ~5 KB: kept off the stack
   std::memset(&p, 0, sizeof(p));
-  st = check_read(c, nodes, n_nodes, p.nodes);
+  bool packed = false;
+  st = check_read(c, nodes, n_nodes, p.nodes, packed_slots ? &packed : nullptr);
   if (st != SVA_OK) return st;
+  p.packed = packed ? c->packed : nullptr;
   p.n_qt = (c->L.T + sva::kTile - 1) / sva::kTile;
   p.nt_slot = c->L.Tpad / sva::kTile;
   st = check_masks(c, nodes, n_nodes, mask);
@@ -1287,6 +1397,12 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
                 Scratch::kWorkspace);
 }
 
+sva_status sva_attend_nodes_packed(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q, void* out,
+                                   float* lse, float scale, const sva_attn_mask* mask, sva_stream s) {
+  return attend(c, nodes, n_nodes, q, out, lse, scale, mask != nullptr ? *mask : sva_attn_mask{}, s,
+                Scratch::kWorkspace, true);
+}
+
 // Attention with the split scratch taken from the library's own device
 // array instead of a caller-attached workspace (see include/sva.h): the same
 // checks, the same split plan and the same kernel as sva_attend_nodes with a
@@ -1488,6 +1604,122 @@ sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_s
   cudaError_t e = sva::launch_condense(p, c->num_sms, reinterpret_cast<cudaStream_t>(s));
   if (e != cudaSuccess) return cuda_fail(e, "condense launch");
   c->slots[dst_slot].resident = true;
+  return ok();
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the calls that move states ask of source i and its destination, in caches that
+// may be one: both exist, the source is written, the destination bound and not given
+// twice, and no source later than where it goes (so that Eq. 4's causality holds there).
+sva_status check_move(const sva_cache* from, const int32_t* src, const sva_cache* to, const int32_t* dst, int32_t i) {
+  const SlotInfo* a = slot_info(from, src[i]);
+  const SlotInfo* b = slot_info(to, dst[i]);
+  if (a == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "source %d: slot %d out of range", i, src[i]);
+  if (b == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "destination %d: slot %d out of range", i, dst[i]);
+  if (!a->bound || !a->resident)
+    return fail(SVA_ERR_NOT_RESIDENT, "source %d: slot %d is %s", i, src[i],
+                a->bound ? "bound but not written" : "not bound");
+  if (!b->bound) return fail(SVA_ERR_INVALID_ARGUMENT, "destination %d: slot %d is not bound", i, dst[i]);
+  for (int32_t k = 0; k < i; ++k)
+    if (dst[k] == dst[i]) return fail(SVA_ERR_INVALID_ARGUMENT, "destinations %d and %d are the same slot %d", k, i, dst[i]);
+  if (a->chunk > b->chunk)
+    return fail(SVA_ERR_CAUSALITY, "source %d holds chunk %d, after its destination's chunk %d", i, a->chunk, b->chunk);
+  return SVA_OK;
+}
+
+sva_status check_moves(const sva_cache* c, const int32_t* src, const int32_t* dst, int32_t n) {
+  if (c == nullptr || src == nullptr || dst == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  if (n < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n %d < 1", n);
+  if (n > SVA_MAX_NODES) return fail(SVA_ERR_CAPACITY, "n %d > SVA_MAX_NODES (%d)", n, SVA_MAX_NODES);
+  return check_device(c);
+}
+
+// sva_cache_pack (pack) and sva_cache_unpack.
+sva_status convert(sva_cache* c, const int32_t* src, const int32_t* dst, int32_t n, bool pack, sva_stream s) {
+  sva_status st = check_moves(c, src, dst, n);
+  if (st != SVA_OK) return st;
+  sva::PackParams p{};
+  for (int32_t i = 0; i < n; ++i) {
+    st = check_move(c, src, c, dst, i);
+    if (st != SVA_OK) return st;
+    const int32_t slot = pack ? src[i] : dst[i], packed = pack ? dst[i] : src[i];
+    if (slot >= SVA_PACKED || packed < SVA_PACKED)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "state %d: slot %d must not be a packed slot and slot %d must be one", i,
+                  slot, packed);
+    const SlotInfo &a = *slot_info(c, src[i]), &b = *slot_info(c, dst[i]);
+    if (a.seq != b.seq)
+      return fail(SVA_ERR_CAUSALITY, "source %d holds a state of sequence %d, its destination is one of %d", i, a.seq,
+                  b.seq);
+    p.slot[i] = slot;
+    p.number[i] = packed - SVA_PACKED;
+  }
+  p.pool = c->base;
+  p.packed = c->packed;
+  p.T = c->L.T;
+  p.Tpad = c->L.Tpad;
+  p.H = c->g.num_heads;
+  p.n = n;
+  cudaError_t e = pack ? sva::launch_pack(p, c->g.head_dim, reinterpret_cast<cudaStream_t>(s))
+                       : sva::launch_unpack(p, c->g.head_dim, reinterpret_cast<cudaStream_t>(s));
+  if (e != cudaSuccess) return cuda_fail(e, pack ? "pack launch" : "unpack launch");
+  for (int32_t i = 0; i < n; ++i) slot_info(c, dst[i])->resident = true;
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+sva_status sva_cache_pack(sva_cache* c, const int32_t* slot, const int32_t* packed, int32_t n, sva_stream s) {
+  return convert(c, slot, packed, n, true, s);
+}
+
+sva_status sva_cache_unpack(sva_cache* c, const int32_t* packed, const int32_t* slot, int32_t n, sva_stream s) {
+  return convert(c, packed, slot, n, false, s);
+}
+
+sva_status sva_cache_copy(sva_cache* from, const int32_t* src_slot, sva_cache* to, const int32_t* dst_slot, int32_t n,
+                          sva_stream s) {
+  sva_status st = check_moves(from, src_slot, dst_slot, n);
+  if (st != SVA_OK) return st;
+  if (to == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
+  st = check_device(to);
+  if (st != SVA_OK) return st;
+  const sva_geometry &a = from->g, &b = to->g;
+  if (a.num_heads != b.num_heads || a.head_dim != b.head_dim || a.frames != b.frames || a.grid_h != b.grid_h ||
+      a.grid_w != b.grid_w || std::memcmp(a.rope_pairs, b.rope_pairs, sizeof(a.rope_pairs)) != 0 ||
+      a.rope_theta != b.rope_theta)
+    return fail(SVA_ERR_INVALID_ARGUMENT,
+                "the caches' states differ (heads, head dimension, frames, grid, rope_pairs or rope_theta)");
+  const bool packed = src_slot[0] >= SVA_PACKED;
+  const size_t slot_bytes = from->L.slot_bytes / a.num_slots, packed_bytes = packed_slot_bytes(a, from->L);
+  sva::StateCopyParams p{};
+  for (int32_t i = 0; i < n; ++i) {
+    st = check_move(from, src_slot, to, dst_slot, i);
+    if (st != SVA_OK) return st;
+    if ((src_slot[i] >= SVA_PACKED) != packed || (dst_slot[i] >= SVA_PACKED) != packed)
+      return fail(SVA_ERR_INVALID_ARGUMENT, "pair %d: the slots of a call are all packed ones, or none is", i);
+    for (int32_t k = 0; from == to && k < n; ++k)
+      if (src_slot[k] == dst_slot[i])
+        return fail(SVA_ERR_INVALID_ARGUMENT, "slot %d is source %d and destination %d", dst_slot[i], k, i);
+    p.src[i] = packed ? from->packed + (size_t)(src_slot[i] - SVA_PACKED) * packed_bytes
+                      : reinterpret_cast<const uint8_t*>(from->base) + (size_t)src_slot[i] * slot_bytes;
+    p.dst[i] = packed ? to->packed + (size_t)(dst_slot[i] - SVA_PACKED) * packed_bytes
+                      : reinterpret_cast<uint8_t*>(to->base) + (size_t)dst_slot[i] * slot_bytes;
+  }
+  // A packed slot is one plane; of a slot the T rows of each K or V and head are one.
+  const size_t row = (size_t)a.head_dim * 2;
+  const size_t plane = packed ? packed_bytes : (size_t)from->L.T * row;
+  p.plane = (uint32_t)(plane / 32);
+  p.vectors = p.plane * (packed ? 1u : 2u * (uint32_t)a.num_heads);  // < 2^28: T <= 2^16, 2^8 planes, 8 of a row
+  p.plane_stride = packed ? 0 : (int64_t)((size_t)from->L.Tpad * row);
+  p.n = n;
+  cudaError_t e = sva::launch_state_copy(p, reinterpret_cast<cudaStream_t>(s));
+  if (e != cudaSuccess) return cuda_fail(e, "state copy launch");
+  for (int32_t i = 0; i < n; ++i) slot_info(to, dst_slot[i])->resident = true;
   return ok();
 }
 

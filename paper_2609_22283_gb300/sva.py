@@ -34,12 +34,16 @@ WITHIN = {"bidirectional": WITHIN_BIDIRECTIONAL, "frame_causal": WITHIN_FRAME_CA
 POLICIES = {"clean": POLICY_CLEAN, "same": POLICY_SAME, "prog": POLICY_PROG}
 MAX_CTX = 16
 MAX_NODES = 64
+PACKED = 1 << 30  # packed slots are numbered from here on
 
 EXPORTED = ("sva_cache_bytes", "sva_cache_create", "sva_cache_bind", "sva_cache_lookup",
             "sva_cache_release", "sva_select_context", "sva_pipeline_round", "sva_check_pipeline",
             "sva_rope_kv_write", "sva_rope_kv_write_qknorm", "sva_rope_kv_write_headnorm",
             "sva_attend_nodes",
             "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_attend_weights", "sva_cache_condense",
+            "sva_packed_bytes", "sva_cache_set_packed", "sva_cache_bind_packed", "sva_cache_lookup_packed",
+            "sva_cache_release_packed", "sva_cache_pack", "sva_cache_unpack", "sva_attend_nodes_packed",
+            "sva_cache_copy",
             "sva_qkv_project",
             "sva_qkv_project_rope",
             "sva_attend_workspace_bytes",
@@ -113,6 +117,15 @@ def load(path: str = LIB_PATH):
         "sva_attend_nodes_masked": ([p, pn, i32, p, p, p, ctypes.c_float, p, p], i32),
         "sva_attend_weights": ([p, pn, i32, p, p, ctypes.c_float, p, p, ctypes.c_float, p, p], i32),
         "sva_cache_condense": ([p, pi32, i32, i32, p, p, p], i32),
+        "sva_packed_bytes": ([pg, i32], ctypes.c_size_t),
+        "sva_cache_set_packed": ([p, p, ctypes.c_size_t, i32], i32),
+        "sva_cache_bind_packed": ([p, i32, i32, i32, pi32], i32),
+        "sva_cache_lookup_packed": ([p, i32, i32, i32, pi32], i32),
+        "sva_cache_release_packed": ([p, i32, i32, i32], i32),
+        "sva_cache_pack": ([p, pi32, pi32, i32, p], i32),
+        "sva_cache_unpack": ([p, pi32, pi32, i32, p], i32),
+        "sva_attend_nodes_packed": ([p, pn, i32, p, p, p, ctypes.c_float, p, p], i32),
+        "sva_cache_copy": ([p, pi32, p, pi32, i32, p], i32),
         "sva_attend_workspace_bytes": ([p], ctypes.c_size_t),
         "sva_attend_nodes_noalloc": ([p, pn, i32, p, p, p, ctypes.c_float, p], i32),
         "sva_cache_set_workspace": ([p, p, ctypes.c_size_t], i32),
@@ -212,6 +225,17 @@ def make_geometry(H, d, F, Hp, Wp, num_slots, pairs, max_frames, theta=10000.0) 
 
 def cache_bytes(g: sva_geometry) -> int:
     return int(load().sva_cache_bytes(ctypes.byref(g)))
+
+
+def packed_bytes(g: sva_geometry, num_packed: int) -> int:
+    n = int(load().sva_packed_bytes(ctypes.byref(g), num_packed))
+    if n == 0:
+        raise SvaError(ERR_INVALID_ARGUMENT, last_error())
+    return n
+
+
+def _slots(slots):
+    return (ctypes.c_int32 * max(len(slots), 1))(*slots)
 
 
 def make_nodes(entries) -> ctypes.Array:
@@ -470,6 +494,64 @@ class Cache:
         n = len(src_slots)
         _check(_lib.sva_cache_condense(self.handle, (ctypes.c_int32 * max(n, 1))(*src_slots), n, dst_slot,
                                        weight.data_ptr(), index.data_ptr(), _stream_handle(stream)))
+
+    def set_packed(self, buf: torch.Tensor | None, num_packed: int = 0):
+        """sva_cache_set_packed: attaches a caller-owned CUDA uint8 tensor of packed_bytes(g, num_packed)
+        as the cache's packed slots, or detaches it."""
+        if buf is not None and (not buf.is_cuda or not buf.is_contiguous()):
+            raise ValueError("packed slots must be a contiguous CUDA tensor")
+        _check(_lib.sva_cache_set_packed(self.handle, buf.data_ptr() if buf is not None else None,
+                                         buf.numel() * buf.element_size() if buf is not None else 0, num_packed))
+        self.packed = buf
+
+    def bind_packed(self, seq: int, chunk: int, level: int) -> int:
+        s = ctypes.c_int32()
+        _check(_lib.sva_cache_bind_packed(self.handle, seq, chunk, level, ctypes.byref(s)))
+        return s.value
+
+    def lookup_packed(self, seq: int, chunk: int, level: int) -> int:
+        s = ctypes.c_int32()
+        _check(_lib.sva_cache_lookup_packed(self.handle, seq, chunk, level, ctypes.byref(s)))
+        return s.value
+
+    def release_packed(self, seq: int, chunk: int, level: int):
+        _check(_lib.sva_cache_release_packed(self.handle, seq, chunk, level))
+
+    def pack(self, slots, packed, stream=None):
+        """sva_cache_pack: the states of `slots` into the packed slots `packed`, in 4 bits."""
+        if len(slots) != len(packed):
+            raise ValueError(f"{len(slots)} slots and {len(packed)} packed slots")
+        _check(_lib.sva_cache_pack(self.handle, _slots(slots), _slots(packed), len(slots), _stream_handle(stream)))
+
+    def unpack(self, packed, slots, stream=None):
+        """sva_cache_unpack: reads the packed slots `packed` into `slots`."""
+        if len(slots) != len(packed):
+            raise ValueError(f"{len(packed)} packed slots and {len(slots)} slots")
+        _check(_lib.sva_cache_unpack(self.handle, _slots(packed), _slots(slots), len(slots), _stream_handle(stream)))
+
+    def copy(self, src_slots, dst_slots, to: Cache | None = None, stream=None):
+        """sva_cache_copy: the states of `src_slots` into `dst_slots` of the cache `to` (None: this one)."""
+        if len(src_slots) != len(dst_slots):
+            raise ValueError(f"{len(src_slots)} sources and {len(dst_slots)} destinations")
+        _check(_lib.sva_cache_copy(self.handle, _slots(src_slots), (self if to is None else to).handle,
+                                   _slots(dst_slots), len(src_slots), _stream_handle(stream)))
+
+    def attend_nodes_packed(self, nodes, q, out, lse=None, scale=None, tile_mask=None, own_mask=None,
+                            hist_mask=None, stream=None, check=True):
+        """sva_attend_nodes_packed: attend_nodes_masked where contexts may be packed slots."""
+        arr, count = _node_array(nodes)
+        if check:
+            _tok_major(q, "q", count, self.T, self.H, self.d)
+            _tok_major(out, "out", count, self.T, self.H, self.d)
+            if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous()
+                                    or lse.shape != (count, self.H, self.T)):
+                raise ValueError("lse must be a contiguous fp32 CUDA tensor [n][H][T]")
+        m = None
+        if tile_mask is not None or own_mask is not None or hist_mask is not None:
+            m = ctypes.byref(self._masks(count, tile_mask, own_mask, hist_mask))
+        _check(_lib.sva_attend_nodes_packed(
+            self.handle, arr, count, q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
+            float(self._scale if scale is None else scale), m, _stream_handle(stream)))
 
     def qkv_project(self, x, weight, bias, q, k, v, stream=None, check=True):
         """sva_qkv_project: [q | k | v] = x W^T + b.  x [..., C] bf16 (rows = all
