@@ -466,14 +466,26 @@ sva_status sva_cache_pack(sva_cache* c, const int32_t* slot, const int32_t* pack
  * conditions and errors otherwise as sva_cache_pack. */
 sva_status sva_cache_unpack(sva_cache* c, const int32_t* packed, const int32_t* slot, int32_t n, sva_stream s);
 
-/* sva_attend_nodes_masked where contexts may be packed slots (own slots are not).  The
- * attention is that over the values which the packed slots stand for: the keys and values are
- * the same as after sva_cache_unpack.  Everything else, masks included, as for
- * sva_attend_nodes_masked; `mask` may be NULL.  A launch without a visible packed context gives
- * the bits of sva_attend_nodes_masked.  Errors: as sva_attend_nodes_masked. */
+/* sva_attend_nodes_masked where contexts may be packed slots (own slots are not): the
+ * attention over the values that the packed slots stand for, the same keys and values as after
+ * sva_cache_unpack.  Everything else, masks included, as for sva_attend_nodes_masked; `mask` may
+ * be NULL.  Without a mask the bits are those of sva_attend_nodes over the states read back;
+ * without a visible packed context they are those of sva_attend_nodes_masked.
+ *   space   device memory into which the launch unpacks the packed states that it reads, before the
+ *           attention itself, if it holds space_bytes >= the number of distinct visible packed contexts
+ *           * 2 * H * Tpad * d * 2 bytes; 256-byte aligned, sharing no memory with anything else of
+ *           the call.  Its contents mean nothing afterwards, so that launches in stream order (of
+ *           several caches) may share it.  NULL or fewer bytes: every work unit unpacks the tiles
+ *           that it reads, which needs no memory and is faster for small launches.
+ * Errors: as sva_attend_nodes_masked, plus INVALID_ARGUMENT for a bad space. */
 sva_status sva_attend_nodes_packed(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q,
                                    void* out, float* lse, float scale, const sva_attn_mask* mask,
-                                   sva_stream s);
+                                   void* space, size_t space_bytes, sva_stream s);
+
+/* Bytes of space with which sva_attend_nodes_packed takes the least time for these nodes: 0 where
+ * that is without one, where no visible context is packed, or where the call would be refused
+ * for its nodes.  Masks are not counted.  Host-side only. */
+size_t sva_attend_packed_space(const sva_cache* c, const sva_node* nodes, int32_t n_nodes);
 
 /* Copies n states in one launch: from src_slot[i] of `from` to dst_slot[i] of `to`, which may
  * be the same cache (a video branches: the states of its sequence copied to those of a new one) or

@@ -19,21 +19,26 @@ cudaError_t configure_d(int dev) {
   // setmaxnreg.inc waits until the block's register pool can serve it: a
   // build whose launch register count leaves the split short would never
   // proceed, so such a build is refused here.
-  for (AttendKernel k :
-       {attend_dense_kernel(D), attend_masked_kernel(D, false), attend_masked_kernel(D, true),
-        attend_cluster_kernel(D, false, false), attend_cluster_kernel(D, true, false),
-        attend_cluster_kernel(D, true, true), attend_packed_kernel(D, false, false),
-        attend_packed_kernel(D, false, true), attend_packed_kernel(D, true, false),
-        attend_packed_kernel(D, true, true)}) {
+  auto ready = [](AttendKernel k, int threads, int pool) {
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          AttnCfg<D>::kSmemBytes);
     if (e != cudaSuccess) return e;
     cudaFuncAttributes fa;
     e = cudaFuncGetAttributes(&fa, k);
     if (e != cudaSuccess) return e;
-    const bool packed = fa.maxThreadsPerBlock == kPackedThreads;
-    const int pool = packed ? AttnRegs<D, true>::kPool : AttnRegs<D>::kPool;
-    if (fa.numRegs * (packed ? kPackedThreads : kThreads) < pool) return cudaErrorInvalidConfiguration;
+    return fa.numRegs * threads < pool ? cudaErrorInvalidConfiguration : cudaSuccess;
+  };
+  for (AttendKernel k :
+       {attend_dense_kernel(D), attend_masked_kernel(D, false), attend_masked_kernel(D, true),
+        attend_cluster_kernel(D, false, false), attend_cluster_kernel(D, true, false),
+        attend_cluster_kernel(D, true, true)}) {
+    cudaError_t e = ready(k, AttnRegs<D>::kThreadsOf, AttnRegs<D>::kPool);
+    if (e != cudaSuccess) return e;
+  }
+  for (int k = 0; k < 4; ++k) {
+    using R = AttnRegs<D, true>;
+    cudaError_t e = ready(attend_packed_kernel(D, (k & 1) != 0, (k & 2) != 0), R::kThreadsOf, R::kPool);
+    if (e != cudaSuccess) return e;
   }
   configured[dev] = true;
   return cudaSuccess;
@@ -48,7 +53,7 @@ cudaError_t launch_d(const AttnParams& p, int grid, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const bool token = p.masked && (p.own_mask != nullptr || p.hist_mask != nullptr);
   const bool packed = p.packed != nullptr;
-  LaunchConfig l(dim3((unsigned)grid), packed ? kPackedThreads : kThreads, AttnCfg<D>::kSmemBytes, s,
+  LaunchConfig l(dim3((unsigned)grid), packed ? AttnRegs<D, true>::kThreadsOf : kThreads, AttnCfg<D>::kSmemBytes, s,
                  p.cluster ? p.n_split : 0);
   AttendKernel k = packed      ? attend_packed_kernel(D, p.masked, p.cluster)
                    : p.cluster ? attend_cluster_kernel(D, p.masked, token)

@@ -123,14 +123,13 @@ __device__ __forceinline__ uint32_t col_o(int b) {
 // 8*32*kRegsHigh <= 384*kLaunchRegs, checked at launch.  At D = 64 a softmax
 // thread holds 128 scores and spills below 216 (88 + 208 was 3% slower).
 //
-// Instances that read packed slots have a fourth warpgroup (warps 12-15), which
-// turns packed tiles into bf16 ones; 512 threads are launched with 128 registers
-// each, and the warpgroups other than the softmax's keep kLow.
+// Instances that read packed slots have a fourth warpgroup (warps 12-15), which turns
+// packed tiles into bf16 ones; every warpgroup but the softmax's keeps kLow registers there.
 constexpr int kThreads = 384;
-constexpr int kPackedThreads = 512;
+constexpr int kUnpackWarps = 4;
 template <int D, bool kPacked = false>
 struct AttnRegs {
-  static constexpr int kThreadsOf = kPacked ? kPackedThreads : kThreads;
+  static constexpr int kThreadsOf = kThreads + (kPacked ? 32 * kUnpackWarps : 0);
   static constexpr int kLaunch = kPacked ? 128 : 168;
   static constexpr int kLow = kPacked ? (D == 128 ? 56 : 40) : (D == 128 ? 88 : 72);
   static constexpr int kHigh = kPacked ? (D == 128 ? 200 : 216) : (D == 128 ? 208 : 216);
@@ -222,7 +221,6 @@ struct PackBars {
   uint64_t k_go[4];
   uint64_t v_go[6];
 };
-constexpr int kUnpackWarps = 4;
 
 // Block-sparse launches: a role's walk over the key tiles that either query
 // tile of the unit may attend (bitmaps in the kernel's tile order).  The
@@ -452,15 +450,18 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
       load_q();
       if (n_tiles > 0) {
         const int st = t_begin / p.nt_slot;
-        if (is_packed(nd.slot[st])) {
+        const int slot = nd.slot[st];
+        if (is_packed(slot)) {
           if constexpr (kPacked) mbar_arrive(&pack.k_go[0]);
         } else {
-          const int row_k = (nd.slot[st] * 2 * p.H + h) * p.Tpad + (t_begin - st * p.nt_slot) * kTile;
+          const CUtensorMap* map = slot >= kSpaceSlot ? &p.tmap_space : &p.tmap_kv;
+          const int row_k =
+              ((slot & (kSpaceSlot - 1)) * 2 * p.H + h) * p.Tpad + (t_begin - st * p.nt_slot) * kTile;
           const uint64_t keep = l2_policy_evict_last();
           expect_tile(&bars.k_full[0]);
 #pragma unroll
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_2d_hint(sK + b * C::kBoxBytes, &p.tmap_kv, &bars.k_full[0], b * 64, row_k, keep);
+            tma_load_2d_hint(sK + b * C::kBoxBytes, map, &bars.k_full[0], b * 64, row_k, keep);
         }
       }
     }
@@ -548,8 +549,10 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
       for (int j = 0; j < n_tiles; ++j, i = sparse ? walk.next() : next_kt(i)) {
         const int ks = j % C::kKStages;
         const int vs = j % C::kVStages;
-        const bool packed = is_packed(nd.slot[i / p.nt_slot]);
-        const int slot = packed ? 0 : nd.slot[i / p.nt_slot];  // (no row of a packed one is worked out)
+        const int from = nd.slot[i / p.nt_slot];
+        const bool packed = is_packed(from);
+        const CUtensorMap* map = from >= kSpaceSlot ? &p.tmap_space : &p.tmap_kv;
+        const int slot = from & (kSpaceSlot - 1);
         const int t = i - (i / p.nt_slot) * p.nt_slot;
         const int row_k = ((slot * 2 + 0) * p.H + h) * p.Tpad + t * kTile;
         const int row_v = row_k + p.H * p.Tpad;
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
             expect_tile(&bars.k_full[ks]);
 #pragma unroll
             for (int b = 0; b < C::kBoxes; ++b)
-              tma_load_2d_hint(sK + ks * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
+              tma_load_2d_hint(sK + ks * C::kTileBytes + b * C::kBoxBytes, map,
                                &bars.k_full[ks], b * 64, row_k, keep);
           }
         }
@@ -586,7 +589,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
             expect_tile(&bars.v_full[vs]);
 #pragma unroll
             for (int b = 0; b < C::kBoxes; ++b)
-              tma_load_2d_hint(sV + vs * C::kTileBytes + b * C::kBoxBytes, &p.tmap_kv,
+              tma_load_2d_hint(sV + vs * C::kTileBytes + b * C::kBoxBytes, map,
                                &bars.v_full[vs], b * 64, row_v, keep);
           }
         }
@@ -798,14 +801,12 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
   } else if (kPacked && warp >= 12) {
     regs_dec<R::kLow>();
     // ------------------------------------------------------------ unpacking
-    // Each warp fills 32 rows of a tile, a thread one: its 4-bit words are loaded a tile
-    // (K or V) ahead, each vector into the registers that the one in front of it has just
-    // left, and go to the stage as the bf16 values that they stand for, in the layout in
-    // which a copy would have put them there.
+    // A thread fills one token's row of a tile with the values that its 4 bits stand for, in
+    // the layout in which a copy would have put them there.  Its words are loaded a tile (K
+    // or V) ahead, each vector into the registers that the one in front of it has just left.
     if constexpr (kPacked) {
-      constexpr int G = D / kPackGroup;  // vectors of 32 elements in a row
-      const int r = (int)threadIdx.x - 384;
-      const uint32_t row_off = (uint32_t)r * 128u, turn = (uint32_t)(r & 7);
+      const int r = (int)threadIdx.x - kThreads;
+      const uint32_t turn = (uint32_t)(r & 7);
       const size_t v_off = (size_t)p.H * p.nt_slot * kPackTileBytes<D>;  // from K to V of a state
       TileWalk<kSparse ? kMaskWords : 1> walk;
       if constexpr (sparse) walk.start(tmask, t_begin, n_all);
@@ -831,32 +832,29 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
         const uint8_t* v_at = at + v_off;
         ++j;
         kt = sparse ? walk.next() : next_kt(kt);
-        const uint8_t* next = seek();
+        at = seek();
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int stages = half ? C::kVStages : C::kKStages;
-          const int s = tile % stages;
+          const int s = tile % (half ? C::kVStages : C::kKStages);
           uint32_t& par = half ? v_par : k_par;
           ok = mbar_wait(half ? &pack.v_go[s] : &pack.k_go[s], (par >> s) & 1u, &abort_flag, tmo);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           par ^= 1u << s;
-          const uint32_t dst = smem_u32(half ? sV : sK) + (uint32_t)s * C::kTileBytes + row_off;
-          // (the last tile loads itself again: in bounds, and not used)
-          const uint8_t* then = half ? (next != nullptr ? next : v_at) : v_at;
+          const uint32_t dst = smem_u32((half ? sV : sK) + s * C::kTileBytes) + (uint32_t)r * 128u;
+          // (behind the last tile its own words are loaded again, for nothing)
+          const uint8_t* then = half && at != nullptr ? at : v_at;
           const typename PackRow<D>::Scales scales = row.scales;
           row.load_scales(then, r);
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
+          for (int g = 0; g < D / kPackGroup; ++g) {
             const uint32_t sc = PackRow<D>::scale(scales, g);
-            const uint4 c = row.codes[g];
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            const uint32_t w[4] = {row.codes[g].x, row.codes[g].y, row.codes[g].z, row.codes[g].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int cc = g * 4 + k;  // 16-byte piece of the row
+              const uint32_t piece = (uint32_t)(g * 4 + k);  // of 16 bytes
               const uint4 x = packed_values(w[k], sc);
-              st_shared_v4(dst + (uint32_t)((cc >> 3) * C::kBoxBytes) + ((((uint32_t)cc & 7u) ^ turn) << 4), x.x, x.y,
-                           x.z, x.w);
+              st_shared_v4(dst + (piece >> 3) * C::kBoxBytes + (((piece & 7u) ^ turn) << 4), x.x, x.y, x.z, x.w);
             }
             row.load_codes(then, r, g);
           }
@@ -864,7 +862,6 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(half ? &bars.v_full[s] : &bars.k_full[s]);
         }
-        at = next;
       }
       if (!ok && lane == 0) record_timeout(p, &abort_flag);
     }

@@ -17,6 +17,7 @@ constexpr int kMaxSplit = 4;  // key-range splits of one work unit, merged throu
 constexpr int kMaxClusterSplit = 8;  // the same, merged inside a thread-block cluster
 constexpr uint64_t kDefaultWaitTimeoutNs = 1000000000ull;  // bounded device waits: 1 s
 constexpr int kPackedSlot = SVA_PACKED;  // slot numbers from here on are packed slots
+constexpr int kSpaceSlot = 1 << 29;      // and from here on states that a launch has unpacked first
 constexpr int kMaskWords = 128;  // block-sparse launches: at most 32 * 128 key tiles per node
 
 // Device status word values (a subset of sva_status).
@@ -29,7 +30,8 @@ struct AttnNode {
   int32_t q_index;
   int32_t n_kv;
   int32_t frame_causal;  // own-chunk keys of later latent frames masked
-  int32_t slot[1 + SVA_MAX_CTX];  // a packed slot (never the own one) as kPackedSlot + its number
+  // kPackedSlot + n: packed slot n; kSpaceSlot + n: state n of the launch's space (never the own one)
+  int32_t slot[1 + SVA_MAX_CTX];
   // key state (0 = own, 1 + j = the caller's ctx_slot[j]) of each entry of
   // `slot`: the row index of its tiles in a block-sparse tile mask
   uint8_t src[1 + SVA_MAX_CTX];
@@ -76,6 +78,7 @@ struct alignas(128) AttnParams {
   int32_t masked;             // a tile or token mask given: a masked kernel instance
   AttnNode nodes[SVA_MAX_NODES];
   const uint8_t* packed;      // packed slots, or null where no node reads one: an instance that does not
+  alignas(128) CUtensorMap tmap_space;  // as tmap_kv, over the launch's space
 };
 
 // Reduction of the token masks to the bytes of AttnParams::any_tile.

@@ -110,7 +110,7 @@ template <int D>
 __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const __grid_constant__ PackParams p) {
   const Place<D> at(p.Tpad);
   ptx::pdl_wait();
-  if (at.token >= p.T) return;
+  if (at.token >= p.T && p.pad == 0) return;  // (a packed slot holds zeros there)
   const uint8_t* tile = at.tile(p, p.number[blockIdx.y]);
   uint32_t c[4];
   uint16_t s;

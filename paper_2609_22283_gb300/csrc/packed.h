@@ -17,6 +17,7 @@
 
 namespace sva {
 
+constexpr int kMaxMoves = SVA_MAX_NODES;  // states of a launch
 constexpr int kPackGroup = 32;  // elements that share a scale
 
 constexpr int pack_tile_bytes(int d) { return kTile * (d / 2 + d / kPackGroup * 2); }
@@ -24,12 +25,13 @@ template <int D>
 constexpr int kPackTileBytes = pack_tile_bytes(D);
 
 struct PackParams {
-  void* pool;       // slot pool base, bf16 [num_slots][2][H][Tpad][d]
+  void* pool;       // slots, bf16 [..][2][H][Tpad][d]
   uint8_t* packed;  // packed slots
   int32_t T, Tpad, H;
   int32_t n;
-  int32_t slot[SVA_MAX_NODES];    // state i: its slot
-  int32_t number[SVA_MAX_NODES];  // and its packed slot, from 0
+  int32_t pad;      // unpacking: 1: the rows past T become zeros too
+  int32_t slot[kMaxMoves];    // state i: its slot
+  int32_t number[kMaxMoves];  // and its packed slot, from 0
 };
 
 // Slots to packed slots, and back (d = 64 or 128).
@@ -41,8 +43,8 @@ struct StateCopyParams {
   uint32_t vectors;      // of a state: all its planes'
   int64_t plane_stride;  // bytes
   int32_t n;
-  const uint8_t* src[SVA_MAX_NODES];
-  uint8_t* dst[SVA_MAX_NODES];
+  const uint8_t* src[kMaxMoves];
+  uint8_t* dst[kMaxMoves];
 };
 
 cudaError_t launch_state_copy(const StateCopyParams& p, cudaStream_t s);

@@ -182,10 +182,10 @@ std::vector<float2> rope_table(int npos, int pairs, double theta) {
   return t;
 }
 
-sva_status encode_2d_kv(CUtensorMap* m, void* base, const sva_geometry& g, const Layout& L) {
+sva_status encode_2d_kv(CUtensorMap* m, void* base, const sva_geometry& g, const Layout& L, int slots) {
   auto fn = encode_fn();
   if (!fn) return fail(SVA_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-  const cuuint64_t rows = (cuuint64_t)g.num_slots * 2 * g.num_heads * L.Tpad;
+  const cuuint64_t rows = (cuuint64_t)slots * 2 * g.num_heads * L.Tpad;
   cuuint64_t dims[2] = {(cuuint64_t)g.head_dim, rows};
   cuuint64_t strides[1] = {(cuuint64_t)g.head_dim * 2};
   cuuint32_t box[2] = {64, (cuuint32_t)sva::kTile};
@@ -660,7 +660,7 @@ sva_status sva_cache_create(const sva_geometry* g, void* dev_buf, size_t bytes, 
     delete c;
     return cuda_fail(e, "cache initialisation");
   }
-  st = encode_2d_kv(&c->tmap_kv, c->base, *g, L);
+  st = encode_2d_kv(&c->tmap_kv, c->base, *g, L, g->num_slots);
   if (st != SVA_OK) {
     delete c;
     return st;
@@ -1023,19 +1023,105 @@ sva_status sva_rope_kv_write_headnorm(sva_cache* c, const sva_node* nodes, int32
 
 namespace {
 
+// Memory of one sva_attend_nodes_packed for the states that it unpacks.
+struct Space {
+  void* data;
+  size_t bytes;
+};
+
+// The distinct packed slots that an attention launch sees, without SVA_PACKED.
+struct PackedReads {
+  int n = 0;
+  long long refs = 0;  // (node, packed slot) pairs
+  int32_t number[SVA_MAX_NODES * SVA_MAX_CTX];
+};
+
+// Lists them; `unpacked`: and makes the nodes read states 0.. of the launch's space in
+// their place, in the list's order.
+void list_packed(const sva_cache* c, sva::AttnNode* nodes, int n_nodes, bool unpacked, PackedReads* r) {
+  // (the scratch of the slot table: a call's own between its entry and its return)
+  std::vector<SlotInfo>& table = const_cast<sva_cache*>(c)->packed_slots;
+  r->n = 0;
+  r->refs = 0;
+  for (int i = 0; i < n_nodes; ++i)
+    for (int k = 1; k < nodes[i].n_kv; ++k) {
+      if (nodes[i].slot[k] < SVA_PACKED) continue;
+      const int32_t number = nodes[i].slot[k] - SVA_PACKED;
+      int32_t& at = table[number].listed;
+      if (at < 0) {
+        at = r->n;
+        r->number[r->n++] = number;
+      }
+      ++r->refs;
+      if (unpacked) nodes[i].slot[k] = sva::kSpaceSlot + at;
+    }
+  for (int i = 0; i < r->n; ++i) table[r->number[i]].listed = -1;
+}
+
+size_t slot_stride(const sva_cache* c) { return c->L.slot_bytes / c->g.num_slots; }
+
+// The first `need` bytes of a launch's space are written while nothing else of the launch
+// has been read: they share no memory with what it reads or writes.
+sva_status check_space(const sva_cache* c, const Space& space, size_t need, const void* q, const void* out,
+                       const float* lse, const sva_attn_mask& m, int n_nodes) {
+  if ((reinterpret_cast<uintptr_t>(space.data) & 255u) != 0)
+    return fail(SVA_ERR_INVALID_ARGUMENT, "space must be 256-byte aligned");
+  if (!on_device(space.data, c->device))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "space is not device memory of the cache's device");
+  const size_t tokens = (size_t)n_nodes * c->L.T, rows = (size_t)n_nodes * (c->L.Tpad / sva::kTile);
+  const size_t act = tokens * c->g.num_heads * c->g.head_dim * 2;
+  const size_t hist_row = std::min((size_t)m.hist_states * (size_t)m.hist_words, (size_t)1 << 40);
+  const struct {
+    const char* name;
+    const void* data;
+    size_t bytes;
+  } others[] = {{"q", q, act},
+                {"out", out, act},
+                {"lse", lse, tokens * c->g.num_heads * sizeof(float)},
+                {"the cache's buffer", c->base, c->L.total},
+                {"the packed slots", c->packed, c->packed_slots.size() * packed_slot_bytes(c->g, c->L)},
+                {"the workspace", c->ws, ws_total_bytes(c)},
+                {"tile_mask", m.tile_mask, m.tile_mask ? rows * m.tile_words * 4 : 0},
+                {"own_mask", m.own_mask, m.own_mask ? tokens * m.own_words * 4 : 0},
+                {"hist_mask", m.hist_mask, m.hist_mask ? tokens * hist_row * 4 : 0}};
+  for (const auto& o : others)
+    if (share_memory(space.data, need, o.data, o.bytes))
+      return fail(SVA_ERR_INVALID_ARGUMENT, "space shares memory with %s", o.name);
+  return SVA_OK;
+}
+
+// Is it faster to unpack a launch's packed states once, before the attention, than in each
+// of its work units?  Estimated in microseconds from measured launches (152 SMs, 64 to 4680
+// tokens, 1 to 40 heads, 1 to 16 packed states):
+//   - by the units: a packed key tile takes a CTA about 0.6 more (d = 64: 0.18), for the
+//     walks of the CTA that has most of them;
+//   - before them: a launch, the states' packed and whole bytes at 8.5 TB/s (the whole ones
+//     stay in L2 for the most part), and what is beyond 64 MB of them read back from HBM.
+// 4680 tokens of 12 heads, three states: 413 us and 329; 320 tokens of 40 heads, sixteen
+// states: 88 and 95; 320 of 12, four: 17.7 and 18.4; 2 x 2160 of 16 x 64, four: 198 and 178.
+bool unpacks_first(const sva_cache* c, const sva::AttnNode* nodes, int n_nodes, const PackedReads& r) {
+  const sva_geometry& g = c->g;
+  const double sms = c->num_sms, nt = c->L.Tpad / sva::kTile, pairs = (c->L.Tpad / sva::kTile + 1) / 2;
+  const double units = (double)n_nodes * g.num_heads * pairs, walks = (double)r.refs * g.num_heads * pairs * nt;
+  const double ctas = std::min(sms, units * std::min<double>(sva::kMaxClusterSplit, std::max(1.0, std::floor(sms / units))));
+  const double whole = (double)r.n * slot_stride(c), packed = (double)r.n * packed_slot_bytes(g, c->L);
+  const double by_units = walks / ctas * (g.head_dim == 128 ? 0.6 : 0.18);
+  return by_units > 2.0 + (whole + packed) / 8.5e6 + std::max(0.0, whole - 64e6) / 6.7e6;
+}
+
 // Where the key-range split partials of an attention launch go.
 enum class Scratch {
   kWorkspace,  // the caller's workspace (sva_cache_set_workspace), if attached
   kStatic,     // the library's static device array (sva_attend_nodes_noalloc)
 };
 
-// sva_attend_nodes, _sparse, _masked, _packed (packed_slots: contexts may be packed
+// sva_attend_nodes, _sparse, _masked, _packed (space not NULL: contexts may be packed
 // slots) and _noalloc: the checks, the launch parameters, the split plan and the
 // launch.  A mask of NULLs is the dense mask.
 // Every check runs before anything is enqueued.
 sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q, void* out,
                   float* lse, float scale, const sva_attn_mask& mask, sva_stream s, Scratch scratch,
-                  bool packed_slots = false) {
+                  const Space* space = nullptr) {
   if (c == nullptr || nodes == nullptr) return fail(SVA_ERR_INVALID_ARGUMENT, "NULL argument");
   if (n_nodes < 1) return fail(SVA_ERR_INVALID_ARGUMENT, "n_nodes %d < 1", n_nodes);
   if (n_nodes > SVA_MAX_NODES)
@@ -1052,9 +1138,8 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
   static thread_local sva::AttnParams p;  // ~5 KB: kept off the stack
   std::memset(&p, 0, sizeof(p));
   bool packed = false;
-  st = check_read(c, nodes, n_nodes, p.nodes, packed_slots ? &packed : nullptr);
+  st = check_read(c, nodes, n_nodes, p.nodes, space != nullptr ? &packed : nullptr);
   if (st != SVA_OK) return st;
-  p.packed = packed ? c->packed : nullptr;
   p.n_qt = (c->L.T + sva::kTile - 1) / sva::kTile;
   p.nt_slot = c->L.Tpad / sva::kTile;
   st = check_masks(c, nodes, n_nodes, mask);
@@ -1149,6 +1234,26 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
     }
   }
 
+  // Packed contexts: unpacked into the launch's space first, where it has room, or by the
+  // attention itself.
+  static thread_local PackedReads reads;
+  reads.n = 0;
+  if (packed) {
+    list_packed(c, p.nodes, n_nodes, false, &reads);
+    const size_t need = (size_t)reads.n * slot_stride(c);
+    const bool unpack = space->data != nullptr && space->bytes >= need &&
+                        (long long)reads.n * 2 * g.num_heads * c->L.Tpad < (1ll << 31);
+    if (unpack) {
+      st = check_space(c, *space, need, q, out, lse, mask, n_nodes);
+      if (st != SVA_OK) return st;
+      st = encode_2d_kv(&p.tmap_space, space->data, g, c->L, reads.n);
+      if (st != SVA_OK) return st;
+      list_packed(c, p.nodes, n_nodes, true, &reads);
+    } else {
+      p.packed = c->packed;
+      reads.n = 0;
+    }
+  }
   if (c->q_cached != q || c->q_cached_n != n_nodes) {
     st = encode_4d_q(&c->tmap_q, q, g, c->L.T, n_nodes);
     if (st != SVA_OK) {
@@ -1192,6 +1297,22 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
     cudaError_t e = launch_scan(c, mask, nodes, n_nodes, max_states, scan_bytes,
                                 reinterpret_cast<cudaStream_t>(s), &p.any_tile, &p.any_stride);
     if (e != cudaSuccess) return cuda_fail(e, "mask scan launch");
+  }
+  for (int at = 0; at < reads.n; at += sva::kMaxMoves) {
+    static thread_local sva::PackParams u;
+    u.pool = static_cast<char*>(space->data) + (size_t)at * slot_stride(c);
+    u.packed = c->packed;
+    u.T = c->L.T;
+    u.Tpad = c->L.Tpad;
+    u.H = g.num_heads;
+    u.n = std::min(reads.n - at, sva::kMaxMoves);
+    u.pad = 1;
+    for (int i = 0; i < u.n; ++i) {
+      u.slot[i] = i;
+      u.number[i] = reads.number[at + i];
+    }
+    cudaError_t e = sva::launch_unpack(u, g.head_dim, reinterpret_cast<cudaStream_t>(s));
+    if (e != cudaSuccess) return cuda_fail(e, "unpack launch");
   }
   const long long grid = n_full + (units - n_full) * n_split;
   cudaError_t e = sva::launch_attend(p, g.head_dim, (int)grid, reinterpret_cast<cudaStream_t>(s));
@@ -1398,9 +1519,21 @@ sva_status sva_attend_nodes_masked(sva_cache* c, const sva_node* nodes, int32_t 
 }
 
 sva_status sva_attend_nodes_packed(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const void* q, void* out,
-                                   float* lse, float scale, const sva_attn_mask* mask, sva_stream s) {
+                                   float* lse, float scale, const sva_attn_mask* mask, void* space,
+                                   size_t space_bytes, sva_stream s) {
+  const Space sp{space, space_bytes};
   return attend(c, nodes, n_nodes, q, out, lse, scale, mask != nullptr ? *mask : sva_attn_mask{}, s,
-                Scratch::kWorkspace, true);
+                Scratch::kWorkspace, &sp);
+}
+
+size_t sva_attend_packed_space(const sva_cache* c, const sva_node* nodes, int32_t n_nodes) {
+  if (c == nullptr || nodes == nullptr || n_nodes < 1 || n_nodes > SVA_MAX_NODES) return 0;
+  static thread_local sva::AttnNode list[SVA_MAX_NODES];
+  bool packed = false;
+  if (check_read(c, nodes, n_nodes, list, &packed) != SVA_OK || !packed) return 0;
+  static thread_local PackedReads reads;
+  list_packed(c, list, n_nodes, false, &reads);
+  return unpacks_first(c, list, n_nodes, reads) ? (size_t)reads.n * slot_stride(c) : 0;
 }
 
 // Attention with the split scratch taken from the library's own device

@@ -43,7 +43,7 @@ EXPORTED = ("sva_cache_bytes", "sva_cache_create", "sva_cache_bind", "sva_cache_
             "sva_attend_nodes_sparse", "sva_attend_nodes_masked", "sva_attend_weights", "sva_cache_condense",
             "sva_packed_bytes", "sva_cache_set_packed", "sva_cache_bind_packed", "sva_cache_lookup_packed",
             "sva_cache_release_packed", "sva_cache_pack", "sva_cache_unpack", "sva_attend_nodes_packed",
-            "sva_cache_copy",
+            "sva_attend_packed_space", "sva_cache_copy",
             "sva_qkv_project",
             "sva_qkv_project_rope",
             "sva_attend_workspace_bytes",
@@ -124,7 +124,8 @@ def load(path: str = LIB_PATH):
         "sva_cache_release_packed": ([p, i32, i32, i32], i32),
         "sva_cache_pack": ([p, pi32, pi32, i32, p], i32),
         "sva_cache_unpack": ([p, pi32, pi32, i32, p], i32),
-        "sva_attend_nodes_packed": ([p, pn, i32, p, p, p, ctypes.c_float, p, p], i32),
+        "sva_attend_nodes_packed": ([p, pn, i32, p, p, p, ctypes.c_float, p, p, ctypes.c_size_t, p], i32),
+        "sva_attend_packed_space": ([p, pn, i32], ctypes.c_size_t),
         "sva_cache_copy": ([p, pi32, p, pi32, i32, p], i32),
         "sva_attend_workspace_bytes": ([p], ctypes.c_size_t),
         "sva_attend_nodes_noalloc": ([p, pn, i32, p, p, p, ctypes.c_float, p], i32),
@@ -537,8 +538,10 @@ class Cache:
                                    _slots(dst_slots), len(src_slots), _stream_handle(stream)))
 
     def attend_nodes_packed(self, nodes, q, out, lse=None, scale=None, tile_mask=None, own_mask=None,
-                            hist_mask=None, stream=None, check=True):
-        """sva_attend_nodes_packed: attend_nodes_masked where contexts may be packed slots."""
+                            hist_mask=None, space=None, stream=None, check=True):
+        """sva_attend_nodes_packed: attend_nodes_masked where contexts may be packed slots.  space: a
+        contiguous CUDA uint8 tensor for the states that are unpacked first (empty: none); None: as much as
+        sva_attend_packed_space says, from torch's allocator, for this call."""
         arr, count = _node_array(nodes)
         if check:
             _tok_major(q, "q", count, self.T, self.H, self.d)
@@ -549,9 +552,21 @@ class Cache:
         m = None
         if tile_mask is not None or own_mask is not None or hist_mask is not None:
             m = ctypes.byref(self._masks(count, tile_mask, own_mask, hist_mask))
+        space_at, nbytes = None, 0
+        if space is None:
+            nbytes = _lib.sva_attend_packed_space(self.handle, arr, count)
+            if nbytes:
+                with torch.cuda.stream(stream):  # the memory is that stream's
+                    space = torch.empty(nbytes, dtype=torch.uint8, device=self.buf.device)
+        elif not space.is_cuda or not space.is_contiguous():
+            raise ValueError("space must be a contiguous CUDA tensor")
+        else:
+            nbytes = space.numel() * space.element_size()
+        if nbytes:
+            space_at = space.data_ptr()
         _check(_lib.sva_attend_nodes_packed(
             self.handle, arr, count, q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
-            float(self._scale if scale is None else scale), m, _stream_handle(stream)))
+            float(self._scale if scale is None else scale), m, space_at, nbytes, _stream_handle(stream)))
 
     def qkv_project(self, x, weight, bias, q, k, v, stream=None, check=True):
         """sva_qkv_project: [q | k | v] = x W^T + b.  x [..., C] bf16 (rows = all

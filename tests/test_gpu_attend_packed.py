@@ -4,9 +4,10 @@ import pytest
 import torch
 
 from paper_2609_22283_gb300.inputs import pack_bits
-from tests._packed import assert_attention, attention, held, make_cache, random_kv, write
+from tests._packed import assert_attention, attention, held, make_cache, random_kv, status, write
 
 pytestmark = pytest.mark.gpu
+NONE = torch.empty(0, dtype=torch.uint8, device="cuda") if torch.cuda.is_available() else None
 
 
 class Layer:
@@ -15,6 +16,7 @@ class Layer:
 
     def __init__(self, sva, F, Hp, Wp, H, d, kinds, nodes=1, causal=False, workspace=True, seed=0, hidden=()):
         W = len(kinds)
+        self.kinds = kinds
         self.F, self.hw, self.T, self.H, self.d, self.n, self.W, self.causal = F, Hp * Wp, F * Hp * Wp, H, d, nodes, W, causal
         self.sva = sva
         c = self.c = make_cache(sva, F, Hp, Wp, H, d, 2 * W + nodes, max(kinds.count("p"), 1), workspace)
@@ -57,6 +59,12 @@ class Layer:
     def buffers(self):
         return (torch.full_like(self.q, float("nan")),
                 torch.full((self.n, self.H, self.T), float("nan"), device="cuda"))
+
+    def space(self, extra=0):
+        """Rubbish, as much as all packed states need (extra: bytes more or less)."""
+        c = self.c
+        n = sum(kind == "p" for kind in self.kinds) * 2 * c.H * c.Tpad * c.d * 2 + extra
+        return torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda")
 
     def run(self, **masks):
         out, lse = self.buffers()
@@ -125,12 +133,12 @@ CASES = [
 @pytest.mark.parametrize("case", range(len(CASES)))
 def test_dense(sva_mod, case):
     """Against the formula, and the same bits as over the states read back (a node's slots in the same order, so the
-    same plan, products and sums)."""
+    same plan, products and sums): unpacked by the units, beforehand, and as the call likes best."""
     a = Layer(sva_mod, seed=case, **CASES[case])
-    out, lse = a.run()
+    out, lse = a.run(space=NONE)
     a.check(out, lse, heads=None if a.H <= 5 else (0, a.H - 1))
-    b_out, b_lse = a.run_back()
-    assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
+    for b_out, b_lse in (a.run_back(), a.run(space=a.space()), a.run(space=a.space(1 << 20)), a.run()):
+        assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
     a.close()
 
 
@@ -168,11 +176,13 @@ def _words(a, b):
 def test_masks(sva_mod, what, case):
     a = Layer(sva_mod, seed=11, **case)
     b = _bools(a, torch.Generator(device="cuda").manual_seed(12), what)
-    out, lse = a.run(**_words(a, b))
+    out, lse = a.run(space=NONE, **_words(a, b))
     a.check(out, lse, heads=(0, a.H - 1), **b)
+    b_out, b_lse = a.run_back(**_words(a, b))
     if what != ("tile",):      # the same instance's arithmetic
-        b_out, b_lse = a.run_back(**_words(a, b))
         assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
+    out, lse = a.run(space=a.space(), **_words(a, b))
+    assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
     a.close()
 
 
@@ -182,8 +192,9 @@ def test_scanned_masks(sva_mod):
     assert 3 * a.H * 7 * 4 * 13 >= 12000
     b = _bools(a, torch.Generator(device="cuda").manual_seed(14), ("own", "hist"))
     b["hist"][:, :512] = False
-    out, lse = a.run(**_words(a, b))
-    a.check(out, lse, heads=(3,), **b)
+    for space in (NONE, a.space()):
+        out, lse = a.run(space=space, **_words(a, b))
+        a.check(out, lse, heads=(3,), **b)
     a.close()
 
 
@@ -238,7 +249,7 @@ def test_repeatable_in_graphs_and_streams(sva_mod):
         with torch.cuda.graph(graph):
             a.c.pack(src, p)                   # what was read back, packed again: the same
             a.c.attend_nodes_packed(a.nodes, a.q, o, l)
-        a.c.packed.zero_()
+        a.c.packed.fill_(255)      # (scales of NaN)
         for _ in range(3):
             o.zero_()
             graph.replay()
@@ -246,7 +257,7 @@ def test_repeatable_in_graphs_and_streams(sva_mod):
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
-            a.c.packed.zero_()
+            a.c.packed.fill_(255)
             a.c.pack(src, p)
             o.zero_()
             a.c.attend_nodes_packed(a.nodes, a.q, o, l)
@@ -266,14 +277,71 @@ def test_timeout(sva_mod, case):
     nothing worse, and the next launch gives the same bits as before."""
     a = Layer(sva_mod, seed=18, **case)
     out, lse = a.run()
-    a.c.debug_inject(1, 0.2)
-    o, l = a.buffers()
-    a.c.attend_nodes_packed(a.nodes, a.q, o, l)
-    assert a.c.poll() == sva_mod.ERR_DEVICE_TIMEOUT
-    a.c.debug_inject(0, 1.0)
-    o, l = a.run()
-    assert torch.equal(o, out) and torch.equal(l, lse)
+    for space in (NONE, a.space()):
+        a.c.debug_inject(1, 0.2)
+        o, l = a.buffers()
+        a.c.attend_nodes_packed(a.nodes, a.q, o, l, space=space)
+        assert a.c.poll() == sva_mod.ERR_DEVICE_TIMEOUT
+        a.c.debug_inject(0, 1.0)
+        o, l = a.run(space=space)
+        assert torch.equal(o, out) and torch.equal(l, lse)
     a.close()
+
+
+def test_space(sva_mod):
+    """A space that is short by a byte is not written; one that overlaps anything of the call or is not aligned is
+    refused; the last key rows behind T are zeros whatever it held."""
+    sva = sva_mod
+    a = Layer(sva, F=1, Hp=9, Wp=15, H=2, d=64, kinds="ppw", seed=20)
+    out, lse = a.run(space=NONE)
+    short = a.space(-1)
+    before = short.clone()
+    o, l = a.run(space=short)
+    assert torch.equal(o, out) and torch.equal(l, lse) and torch.equal(short, before)
+    full = torch.full_like(a.space(), 255)          # bf16 NaN
+    o, l = a.run(space=full)
+    assert torch.equal(o, out) and torch.equal(l, lse)
+    n = full.numel()
+    need = torch.full((n + 512,), 255, dtype=torch.uint8, device="cuda")
+    bad = sva.ERR_INVALID_ARGUMENT
+
+    def call(space, q=a.q, out=out, **kw):
+        return status(lambda: a.c.attend_nodes_packed(a.nodes, q, out, space=space, **kw))
+
+    assert call(need[16:n + 16]) == bad
+    whole = torch.empty(n + a.q.numel() * 2, dtype=torch.uint8, device="cuda")
+    inside = whole[n - 256:n - 256 + a.q.numel() * 2].view(torch.bfloat16).view(a.q.shape)
+    inside.copy_(a.q)
+    kept = whole.clone()
+    assert call(whole[:n], q=inside) == bad and "q" in sva.last_error()
+    assert call(whole[:n], out=inside) == bad and "out" in sva.last_error()
+    assert torch.equal(whole, kept)
+    assert call(a.c.ws[256:256 + n]) == bad
+    assert call(whole[:n], own_mask=whole[:4 * a.T * 5].view(torch.int32).view(1, a.T, 5)) == bad
+    lib = sva.load()
+    host = torch.empty(n + 256, dtype=torch.uint8)
+    at = (host.data_ptr() + 255) // 256 * 256
+    assert lib.sva_attend_nodes_packed(a.c.handle, a.nodes, 1, a.q.data_ptr(), out.data_ptr(), None, 0.125, None, at, n,
+                                       0) == bad
+    assert a.c.poll() == sva.OK
+    a.close()
+
+
+def test_advice(sva_mod):
+    """Full chunks are unpacked first, small launches by their units, and nothing where nothing is packed or seen; the
+    call takes what it is advised."""
+    lib = sva_mod.load()
+    for want, case in ((3, dict(F=3, Hp=30, Wp=52, H=4, d=128, kinds="pppw", nodes=2)), (0, dict(F=1, Hp=16, Wp=20, H=4, d=128, kinds="pp")),
+                       (0, dict(F=3, Hp=30, Wp=52, H=2, d=64, kinds="ww")),
+                       (0, dict(F=3, Hp=30, Wp=52, H=2, d=64, kinds="pp", hidden=(0, 1)))):
+        a = Layer(sva_mod, seed=21, **case)
+        c = a.c
+        assert lib.sva_attend_packed_space(c.handle, a.nodes, a.n) == want * 2 * c.H * c.Tpad * c.d * 2
+        out, lse = a.run()
+        b_out, b_lse = a.run_back()
+        assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
+        a.close()
+    assert lib.sva_attend_packed_space(None, None, 1) == 0
 
 
 def test_full_chunks(sva_mod):

@@ -109,4 +109,5 @@ def test_null_arguments_without_a_gpu(sva_mod):
     assert lib.sva_cache_pack(None, one, one, 1, None) == bad
     assert lib.sva_cache_unpack(None, one, one, 1, None) == bad
     assert lib.sva_cache_copy(None, one, None, one, 1, None) == bad
-    assert lib.sva_attend_nodes_packed(None, None, 1, None, None, None, 0.125, None, None) == bad
+    assert lib.sva_attend_nodes_packed(None, None, 1, None, None, None, 0.125, None, None, 0, None) == bad
+    assert lib.sva_attend_packed_space(None, None, 1) == 0
