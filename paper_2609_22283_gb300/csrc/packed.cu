@@ -18,6 +18,7 @@ namespace sva {
 namespace {
 
 constexpr int kPackThreads = 256;
+constexpr uint32_t kZeroCodes = 0x44444444u;  // eight codes of 0: 8 in each four bits, turned by 3
 
 struct Words16 {
   uint32_t w[16];
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
   const Place<D> at(p.Tpad);
   ptx::pdl_wait();
   uint8_t* tile = at.tile(p, p.number[blockIdx.y]);
-  uint32_t codes[4] = {0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u};
+  uint32_t codes[4] = {kZeroCodes, kZeroCodes, kZeroCodes, kZeroCodes};
   uint32_t scale = 0;
   if (at.token < p.T) {
     const Words16 x = ld_group(at.row(p, p.slot[blockIdx.y]));
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
         const float hi = __fmaf_rn(__uint_as_float(v & 0xFFFF0000u), inv, 0x1p23f + 8.0f);
         w = (w << 4) + __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
       }
-      codes[k] = s > 0.0f ? w : 0x88888888u;
+      codes[k] = s > 0.0f ? __funnelshift_l(w, w, 3) : kZeroCodes;
     }
   }
   *reinterpret_cast<uint4*>(tile + at.codes_at()) = make_uint4(codes[0], codes[1], codes[2], codes[3]);

@@ -13,11 +13,13 @@ namespace sva {
 // code * scale = (16 + n) * scale - 24 * scale.  A scale has at most 5 significant
 // bits and is below 2^122, so 24 * scale (3 * 2^3) and the result (at most 7 of 3
 // bits) are bf16 numbers: the fused multiply-add rounds nothing.  Three instructions
-// a pair.
+// a pair, two for the first: inside the attention it is their number that counts (with
+// words not turned, one shift more of four, 4680 queries over three packed states of 12
+// heads took 418 us instead of 384).
 __device__ __forceinline__ uint4 packed_values(uint32_t w, uint32_t scale) {
   uint32_t off, o[4];
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(scale), "r"(0xC1C0C1C0u));  // -24
-  const uint32_t at[4] = {w << 3, w >> 1, w >> 5, w >> 9};
+  const uint32_t at[4] = {w, w >> 4, w >> 8, __funnelshift_r(w, w, 12)};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t v = (at[j] & 0x00780078u) | 0x41804180u;  // 16 + n

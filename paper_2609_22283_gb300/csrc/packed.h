@@ -7,10 +7,11 @@
 // so that the threads that take a tile's tokens one each read whole lines, and a
 // tile is one piece of memory.  Tokens past T have scale 0.
 //
-// Byte order of a group: 32-bit word k holds elements 8k..8k+7; element 8k + 2j has
-// the four bits from 4j on, element 8k + 2j + 1 those from 16 + 4j on, each as its
-// code + 8 (1..15).  So a shift and a mask leave two neighbouring elements in the two
-// halves of a word (packed_values in packed.cuh).
+// Bit order of a group: 32-bit word k holds elements 8k..8k+7; element 8k + 2j has the
+// four bits from 4j on, element 8k + 2j + 1 those from 16 + 4j on, each as its code + 8
+// (1..15), and the word is turned left by 3.  So a shift (none for the first pair) and a
+// mask leave two neighbouring elements in the two halves of a word, behind the place of a
+// bf16 number's exponent (packed_values in packed.cuh).
 #pragma once
 
 #include "internal.h"
