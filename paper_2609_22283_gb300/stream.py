@@ -1,6 +1,7 @@
-"""One attention layer over a video that outgrows its cache.
+"""One attention layer over a video that outgrows its cache, in two ways: Stream condenses old states,
+PackedStream holds them in 4 bits.
 
-Chunks come one after the other under clean history (every node reads level-0
+Stream.  Chunks come one after the other under clean history (every node reads level-0
 states of earlier chunks).  The last `window` clean states are kept whole; when
 one more is written, the oldest ones are condensed: head by head, the tokens that
 got the most attention so far stay, in one state of a chunk's size, which every
@@ -84,6 +85,108 @@ class Stream:
         for chunk, _ in old:
             c.release(0, chunk, 0)
         self.condensed = (newest, dst)
+
+    def close(self):
+        self.cache.close()
+
+
+class PackedStream:
+    """A layer that keeps a longer window: of its clean states the newest `recent` are whole, the others are held in 4
+    bits, and the oldest one goes when a new one comes.  A video may branch: from fork() on, two sequences go on from
+    the same history, each with updates of its own.
+
+    One update of a chunk: sva_rope_kv_write_headnorm into the chunk's own slot, sva_attend_nodes_packed over the
+    sequence's history and the own chunk, and after a clean refresh (level 0) sva_cache_pack of the state that leaves
+    the newest ones.  fork() is sva_cache_copy of whole and of packed states."""
+
+    def __init__(self, H, d, F, Hp, Wp, pairs, max_frames, window=12, recent=2, sequences=1, theta=10000.0, device="cuda"):
+        """window: clean states that an update reads, up to MAX_CTX; recent: how many of them stay whole (0..window);
+        sequences: how many there may be at once."""
+        if not 0 <= recent <= window <= sva.MAX_CTX or window < 1 or sequences < 1:
+            raise ValueError(f"need 0 <= recent <= window, 1 <= window <= {sva.MAX_CTX} and sequences >= 1")
+        g = sva.make_geometry(H, d, F, Hp, Wp, num_slots=sequences * recent + 1, pairs=pairs, max_frames=max_frames,
+                              theta=theta)
+        self.cache = sva.Cache(g, device=device)
+        c, self.device = self.cache, self.cache.buf.device
+        c.set_workspace(torch.empty(c.workspace_bytes(), dtype=torch.uint8, device=self.device))
+        if window > recent:
+            n = sequences * (window - recent)
+            c.set_packed(torch.empty(sva.packed_bytes(g, n), dtype=torch.uint8, device=self.device), n)
+        self.window, self.recent, self.sequences = window, recent, sequences
+        self.whole = {0: []}   # sequence -> [(chunk, slot)], oldest first
+        self.packed = {0: []}  # and the packed ones before them
+
+    def context(self, seq=0):
+        """The slots that the next update of the sequence reads, oldest first."""
+        return [s for _, s in self.packed[seq] + self.whole[seq]]
+
+    def update(self, chunk, level, q, k, v, out, gamma_k=None, gamma_q=None, eps=1e-6, seq=0):
+        """One update of a chunk, arguments as Stream.update.  One that raises before its attention is launched leaves
+        no state behind, so that it can be made again."""
+        c, context = self.cache, self.context(seq)
+        slot = c.bind(seq, chunk, level)
+        try:
+            node = sva.make_nodes([dict(seq=seq, chunk=chunk, level=level, own_slot=slot, ctx=context)])
+            rotated = torch.empty_like(out)
+            c.rope_kv_write_headnorm(node, k, v, q, rotated, gamma_k, gamma_q, eps)
+            c.attend_nodes_packed(node, rotated, out)
+        except BaseException:
+            c.release(seq, chunk, level)
+            raise
+        if level != 0:
+            c.release(seq, chunk, level)
+            return
+        self.whole[seq].append((chunk, slot))
+        if len(self.whole[seq]) > self.recent:
+            self._park(seq)
+
+    def _park(self, seq):
+        c, whole, packed = self.cache, self.whole[seq], self.packed[seq]
+        chunk, slot = whole[0]
+        if self.window > self.recent:
+            if len(packed) == self.window - self.recent:
+                c.release_packed(seq, packed[0][0], 0)
+                del packed[0]
+            at = c.bind_packed(seq, chunk, 0)
+            try:
+                c.pack([slot], [at])
+            except BaseException:
+                c.release_packed(seq, chunk, 0)
+                raise
+            packed.append((chunk, at))
+        c.release(seq, chunk, 0)
+        del whole[0]
+
+    def fork(self, seq, new):
+        """A new sequence `new` with the history of `seq`."""
+        if seq not in self.whole or new in self.whole:
+            raise ValueError(f"sequence {seq} must exist and {new} must not")
+        if len(self.whole) == self.sequences:
+            raise ValueError(f"there are {self.sequences} sequences already")
+        c, done = self.cache, []
+        try:
+            for old, bind, release in ((self.whole[seq], c.bind, c.release),
+                                       (self.packed[seq], c.bind_packed, c.release_packed)):
+                copies = []
+                for chunk, _ in old:
+                    copies.append((chunk, bind(new, chunk, 0)))
+                    done.append((release, chunk))
+                if copies:
+                    c.copy([s for _, s in old], [s for _, s in copies])
+                (self.whole if old is self.whole[seq] else self.packed)[new] = copies
+        except BaseException:
+            for release, chunk in done:
+                release(new, chunk, 0)
+            self.whole.pop(new, None)
+            self.packed.pop(new, None)
+            raise
+
+    def drop(self, seq):
+        """Lets a sequence and its states go."""
+        for chunk, _ in self.whole.pop(seq):
+            self.cache.release(seq, chunk, 0)
+        for chunk, _ in self.packed.pop(seq):
+            self.cache.release_packed(seq, chunk, 0)
 
     def close(self):
         self.cache.close()
