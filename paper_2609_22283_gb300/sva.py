@@ -235,10 +235,6 @@ def packed_bytes(g: sva_geometry, num_packed: int) -> int:
     return n
 
 
-def _slots(slots):
-    return (ctypes.c_int32 * max(len(slots), 1))(*slots)
-
-
 def make_nodes(entries) -> ctypes.Array:
     """entries: iterable of dicts with seq, chunk, level, own_slot, ctx (list of slots),
     visible (optional list of 0/1), within (optional, default bidirectional)."""
@@ -284,7 +280,9 @@ class Cache:
         self.T = g.frames * g.grid_h * g.grid_w
         self.Tpad = (self.T + 127) // 128 * 128
         self._w_shape = (int(g.num_slots), self.H, self.T)
-        # arguments of rope_kv_write_headnorm, made once (a cache has one host thread at a time)
+        # arguments of rope_kv_write_headnorm and of the calls that move states, made once (a cache has one
+        # host thread at a time; two arrays of slots made anew cost 1.5 us of a call, filled 0.3)
+        self._moves = [(ctypes.c_int32 * MAX_NODES)() for _ in range(2)]
         self._rows = [sva_token_rows() for _ in range(3)]
         self._rows_at = [ctypes.byref(r) for r in self._rows]
         handle = ctypes.c_void_p()
@@ -518,24 +516,31 @@ class Cache:
     def release_packed(self, seq: int, chunk: int, level: int):
         _check(_lib.sva_cache_release_packed(self.handle, seq, chunk, level))
 
+    def _move(self, src, dst):
+        """(sources, destinations, their number) of a call that moves states."""
+        n = len(src)
+        if n != len(dst):
+            raise ValueError(f"{n} sources and {len(dst)} destinations")
+        if n > MAX_NODES:  # which the call refuses
+            return (ctypes.c_int32 * n)(*src), (ctypes.c_int32 * n)(*dst), n
+        a, b = self._moves
+        a[:n], b[:n] = src, dst
+        return a, b, n
+
     def pack(self, slots, packed, stream=None):
         """sva_cache_pack: the states of `slots` into the packed slots `packed`, in 4 bits."""
-        if len(slots) != len(packed):
-            raise ValueError(f"{len(slots)} slots and {len(packed)} packed slots")
-        _check(_lib.sva_cache_pack(self.handle, _slots(slots), _slots(packed), len(slots), _stream_handle(stream)))
+        a, b, n = self._move(slots, packed)
+        _check(_lib.sva_cache_pack(self.handle, a, b, n, _stream_handle(stream)))
 
     def unpack(self, packed, slots, stream=None):
         """sva_cache_unpack: reads the packed slots `packed` into `slots`."""
-        if len(slots) != len(packed):
-            raise ValueError(f"{len(packed)} packed slots and {len(slots)} slots")
-        _check(_lib.sva_cache_unpack(self.handle, _slots(packed), _slots(slots), len(slots), _stream_handle(stream)))
+        a, b, n = self._move(packed, slots)
+        _check(_lib.sva_cache_unpack(self.handle, a, b, n, _stream_handle(stream)))
 
     def copy(self, src_slots, dst_slots, to: Cache | None = None, stream=None):
         """sva_cache_copy: the states of `src_slots` into `dst_slots` of the cache `to` (None: this one)."""
-        if len(src_slots) != len(dst_slots):
-            raise ValueError(f"{len(src_slots)} sources and {len(dst_slots)} destinations")
-        _check(_lib.sva_cache_copy(self.handle, _slots(src_slots), (self if to is None else to).handle,
-                                   _slots(dst_slots), len(src_slots), _stream_handle(stream)))
+        a, b, n = self._move(src_slots, dst_slots)
+        _check(_lib.sva_cache_copy(self.handle, a, (self if to is None else to).handle, b, n, _stream_handle(stream)))
 
     def attend_nodes_packed(self, nodes, q, out, lse=None, scale=None, tile_mask=None, own_mask=None,
                             hist_mask=None, space=None, stream=None, check=True):
