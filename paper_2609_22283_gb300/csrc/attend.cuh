@@ -833,7 +833,10 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
         ++j;
         kt = sparse ? walk.next() : next_kt(kt);
         at = seek();
-#pragma unroll
+        // D = 128: K and V by one piece of code, as the warps of an SM sub-partition run four
+        // kinds of loops and wait for instructions (small launches 4% slower with two; at D
+        // = 64 8% faster).
+#pragma unroll(D == 128 ? 1 : 2)
         for (int half = 0; half < 2; ++half) {
           const int s = tile % (half ? C::kVStages : C::kKStages);
           uint32_t& par = half ? v_par : k_par;

@@ -1093,19 +1093,19 @@ sva_status check_space(const sva_cache* c, const Space& space, size_t need, cons
 // Is it faster to unpack a launch's packed states once, before the attention, than in each
 // of its work units?  Estimated in microseconds from measured launches (152 SMs, 64 to 4680
 // tokens, 1 to 40 heads, 1 to 16 packed states):
-//   - by the units: a packed key tile takes a CTA about 0.5 more (d = 64: 0.15), for the
+//   - by the units: a packed key tile takes a CTA about 0.43 more (d = 64: 0.15), for the
 //     walks of the CTA that has most of them;
 //   - before them: a launch, the states' packed and whole bytes at 8.5 TB/s (the whole ones
 //     stay in L2 for the most part), and what is beyond 64 MB of them read back from HBM.
-// 4680 tokens of 12 heads, three states: 384 us and 329; 320 tokens of 40 heads, sixteen
-// states: 85 and 95; 320 of 12, four: 17.5 and 18.4; 2 x 2160 of 16 x 64, four: 198 and 178.
+// 4680 tokens of 12 heads, three states: 381 us and 329; 320 tokens of 40 heads, sixteen
+// states: 84 and 95; 320 of 12, four: 16.7 and 18.4; 2 x 2160 of 16 x 64, four: 195 and 178.
 bool unpacks_first(const sva_cache* c, const sva::AttnNode* nodes, int n_nodes, const PackedReads& r) {
   const sva_geometry& g = c->g;
   const double sms = c->num_sms, nt = c->L.Tpad / sva::kTile, pairs = (c->L.Tpad / sva::kTile + 1) / 2;
   const double units = (double)n_nodes * g.num_heads * pairs, walks = (double)r.refs * g.num_heads * pairs * nt;
   const double ctas = std::min(sms, units * std::min<double>(sva::kMaxClusterSplit, std::max(1.0, std::floor(sms / units))));
   const double whole = (double)r.n * slot_stride(c), packed = (double)r.n * packed_slot_bytes(g, c->L);
-  const double by_units = walks / ctas * (g.head_dim == 128 ? 0.5 : 0.15);
+  const double by_units = walks / ctas * (g.head_dim == 128 ? 0.43 : 0.15);
   return by_units > 2.0 + (whole + packed) / 8.5e6 + std::max(0.0, whole - 64e6) / 6.7e6;
 }
 
