@@ -468,7 +468,7 @@ sva_status sva_cache_unpack(sva_cache* c, const int32_t* packed, const int32_t* 
 
 /* sva_attend_nodes_masked where contexts may be packed slots (own slots are not): the
  * attention over the values that the packed slots stand for, the same keys and values as after
- * sva_cache_unpack.  Everything else, masks included, as for sva_attend_nodes_masked; `mask` may
+ * sva_cache_unpack.  A node lists a state once, whole or packed.  Everything else, masks included, as for sva_attend_nodes_masked; `mask` may
  * be NULL.  Without a mask the bits are those of sva_attend_nodes over the states read back;
  * without a visible packed context they are those of sva_attend_nodes_masked.
  *   space   device memory into which the launch unpacks the packed states that it reads, before the
@@ -495,8 +495,8 @@ size_t sva_attend_packed_space(const sva_cache* c, const sva_node* nodes, int32_
  *   dst_slot  distinct slots, bound by the caller to states of any sequence whose chunk is not
  *             before the source's; none of them a source of the same call
  *   n         1..SVA_MAX_NODES
- * The caches agree in everything that a state's rows depend on: heads, head dimension, frames,
- * grid, rope_pairs, rope_theta.  Stream-ordered (both caches' calls on the one stream).  Errors:
+ * The caches share no memory and agree in everything that a state's rows depend on: heads, head
+ * dimension, frames, grid, rope_pairs, rope_theta.  Stream-ordered (both caches' calls on the one stream).  Errors:
  * INVALID_ARGUMENT, NOT_RESIDENT (a source), CAUSALITY (an earlier chunk than the source's),
  * CAPACITY (n), CUDA. */
 sva_status sva_cache_copy(sva_cache* from, const int32_t* src_slot, sva_cache* to, const int32_t* dst_slot,

@@ -826,9 +826,13 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
       PackRow<D> row;
       if (at != nullptr) row.load_all(at, r);
       uint32_t k_par = 0, v_par = 0;  // phase of each stage's go barrier
+      int last = -1;                  // the tile before
       bool ok = true;
       while (ok && at != nullptr) {
         const int tile = j;
+        // the unpacked tiles in front of it have a wait's time each
+        const uint64_t limit = tmo * (uint64_t)(tile - last);
+        last = tile;
         const uint8_t* v_at = at + v_off;
         ++j;
         kt = sparse ? walk.next() : next_kt(kt);
@@ -840,7 +844,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
         for (int half = 0; half < 2; ++half) {
           const int s = tile % (half ? C::kVStages : C::kKStages);
           uint32_t& par = half ? v_par : k_par;
-          ok = mbar_wait(half ? &pack.v_go[s] : &pack.k_go[s], (par >> s) & 1u, &abort_flag, tmo);
+          ok = mbar_wait(half ? &pack.v_go[s] : &pack.k_go[s], (par >> s) & 1u, &abort_flag, limit);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           par ^= 1u << s;

@@ -12,6 +12,7 @@
 #include <cstdio>
 #include <cstring>
 #include <map>
+#include <new>
 #include <string>
 #include <tuple>
 #include <vector>
@@ -353,6 +354,12 @@ sva_status check_read(const sva_cache* c, const sva_node* nodes, int n_nodes, sv
       for (int k2 = 0; k2 < k; ++k2)
         if (n.ctx_slot[k2] == cs)
           return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: slot %d listed twice", i, cs);
+      for (int k2 = 0; packed != nullptr && k2 < k; ++k2) {
+        const SlotInfo& other = *slot_info(c, n.ctx_slot[k2]);  // (of the same sequence)
+        if (other.chunk == si.chunk && other.level == si.level)
+          return fail(SVA_ERR_INVALID_ARGUMENT, "node %d: slots %d and %d hold the same state (chunk %d, level %d)", i,
+                      n.ctx_slot[k2], cs, si.chunk, si.level);
+      }
       if (n.ctx_visible[k]) {
         a.src[nkv] = (uint8_t)(1 + k);
         a.slot[nkv++] = cs;
@@ -742,10 +749,17 @@ sva_status sva_cache_set_packed(sva_cache* c, void* dev_buf, size_t bytes, int32
         share_memory(dev_buf, need, c->ws, c->ws != nullptr ? ws_total_bytes(c) : 0))
       return fail(SVA_ERR_INVALID_ARGUMENT, "packed slots share memory with the cache's buffer or its workspace");
   }
+  const int32_t n = dev_buf != nullptr ? num_packed : 0;
+  try {
+    std::vector<SlotInfo> slots(n);
+    std::vector<int32_t> free_slots(n);
+    for (int32_t i = 0; i < n; ++i) free_slots[i] = n - 1 - i;
+    c->packed_slots.swap(slots);
+    c->packed_free.swap(free_slots);
+  } catch (const std::bad_alloc&) {
+    return fail(SVA_ERR_CAPACITY, "no host memory for the table of %d packed slots", n);
+  }
   c->packed = static_cast<uint8_t*>(dev_buf);
-  c->packed_slots.assign(dev_buf != nullptr ? num_packed : 0, SlotInfo());
-  c->packed_free.clear();
-  for (int32_t s = (int32_t)c->packed_slots.size() - 1; s >= 0; --s) c->packed_free.push_back(s);
   return ok();
 }
 
@@ -760,6 +774,11 @@ sva_status sva_cache_bind_packed(sva_cache* c, int32_t seq, int32_t chunk, int32
   if (c->packed_free.empty())
     return fail(SVA_ERR_CAPACITY, "all %zu packed slots are bound", c->packed_slots.size());
   const int32_t s = c->packed_free.back();
+  try {
+    c->packed_index.emplace(k, s);
+  } catch (const std::bad_alloc&) {
+    return fail(SVA_ERR_CAPACITY, "no host memory for another packed slot");
+  }
   c->packed_free.pop_back();
   SlotInfo& si = c->packed_slots[s];
   si.bound = true;
@@ -767,7 +786,6 @@ sva_status sva_cache_bind_packed(sva_cache* c, int32_t seq, int32_t chunk, int32
   si.seq = seq;
   si.chunk = chunk;
   si.level = level;
-  c->packed_index[k] = s;
   *slot = SVA_PACKED + s;
   return ok();
 }
@@ -1827,8 +1845,12 @@ sva_status sva_cache_copy(sva_cache* from, const int32_t* src_slot, sva_cache* t
       a.rope_theta != b.rope_theta)
     return fail(SVA_ERR_INVALID_ARGUMENT,
                 "the caches' states differ (heads, head dimension, frames, grid, rope_pairs or rope_theta)");
+  const size_t slot_bytes = slot_stride(from), packed_bytes = packed_slot_bytes(a, from->L);
+  if (from != to && (share_memory(from->base, from->L.total, to->base, to->L.total) ||
+                     share_memory(from->packed, from->packed_slots.size() * packed_bytes, to->packed,
+                                  to->packed_slots.size() * packed_bytes)))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "the two caches share memory");
   const bool packed = src_slot[0] >= SVA_PACKED;
-  const size_t slot_bytes = from->L.slot_bytes / a.num_slots, packed_bytes = packed_slot_bytes(a, from->L);
   sva::StateCopyParams p{};
   for (int32_t i = 0; i < n; ++i) {
     st = check_move(from, src_slot, to, dst_slot, i);

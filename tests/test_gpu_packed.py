@@ -177,6 +177,11 @@ def test_refusals(sva_mod):
     c.release_packed(0, 6, 0)
     far = c.bind_packed(0, 12, 0)
     c.pack([own], [far])
+    c.release_packed(0, 5, 1)
+    again = c.bind_packed(0, 5, 0)
+    c.pack([a], [again])
+    assert call(ctx=[a, again]) == bad and call(ctx=[again, a]) == bad       # one state, whole and packed
+    assert "same state" in sva.last_error()
     assert call(ctx=[far]) == causal
     torch.cuda.synchronize()
     assert (out == 7.0).all()
@@ -184,7 +189,7 @@ def test_refusals(sva_mod):
     small = torch.empty(sva.packed_bytes(c.g, 2), dtype=torch.uint8, device="cuda")
     assert status(lambda: c.set_packed(small, 2)) == bad                   # slots are bound
     assert status(lambda: c.set_packed(None)) == bad
-    for s in ((0, 5, 1), (1, 9, 0), (0, 12, 0)):
+    for s in ((0, 5, 0), (1, 9, 0), (0, 12, 0)):
         c.release_packed(*s)
     assert status(lambda: c.set_packed(small, 3)) == bad                   # too small
     assert status(lambda: c.set_packed(small, 0)) == bad
@@ -272,6 +277,13 @@ def test_copy_refusals(sva_mod):
     t = other.bind(0, 5, 0)
     assert status(lambda: c.copy([a], [t], to=other)) == bad
     other.close()
+    twin = sva.Cache(c.g, buf=torch.empty(2 * c.nbytes, dtype=torch.uint8, device="cuda"))
+    t = twin.bind(0, 5, 0)
+    twin.set_packed(c.packed, 1)
+    assert status(lambda: c.copy([a], [t], to=twin)) == bad and "share" in sva.last_error()
+    twin.set_packed(None)
+    c.copy([a], [t], to=twin)
+    twin.close()
     torch.cuda.synchronize()
     assert torch.equal(before.view(torch.int16), c.slot_pool().view(torch.int16))
     c.close()
