@@ -352,3 +352,52 @@ def test_full_chunks(sva_mod):
     b_out, b_lse = a.run_back()
     assert torch.equal(out, b_out) and torch.equal(lse, b_lse)
     a.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_longest_chunk(sva_mod, d):
+    """65536 tokens, 512 tiles a state: queries of the first, a middle and the last tile against the formula."""
+    a = Layer(sva_mod, F=1, Hp=256, Wp=256, H=1, d=d, kinds="p", seed=22)
+    rows = torch.cat([torch.arange(r, r + 40, device="cuda") for r in (0, 32700, 65496)])
+    k, v = (torch.cat([a.kv[s][x, 0].double() for s in a.see[0]]) for x in (0, 1))
+    ref = attention(a.q[0, rows, 0], k, v)
+    outs = [a.run(space=NONE), a.run(space=a.space())]
+    for out, lse in outs:
+        assert_attention(out[0, rows, 0], lse[0, 0, rows], ref)
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    a.close()
+
+
+def test_most_nodes_and_contexts(sva_mod):
+    """64 nodes of one token with sixteen contexts each, eighty distinct packed states among them: more than one
+    launch unpacks at a time."""
+    sva, H, d = sva_mod, 1, 64
+    c = make_cache(sva, 1, 1, 1, H, d, 64 + 1, 80, chunks=200)
+    g = torch.Generator(device="cuda").manual_seed(23)
+    kv, packed = [], []
+    for i in range(80):
+        x = random_kv(c, g)
+        s = write(c, (0, 1 + i, 0), x)
+        packed.append(c.bind_packed(0, 1 + i, 0))
+        c.pack([s], [packed[i]])
+        c.release(0, 1 + i, 0)
+        kv.append(held(x))
+    nodes, own = [], []
+    for i in range(64):
+        x = random_kv(c, g)
+        own.append(x)
+        nodes.append(dict(seq=0, chunk=100 + i, level=0, own_slot=write(c, (0, 100 + i, 0), x),
+                          ctx=[packed[(5 * i + k) % 80] for k in range(16)]))
+    q = torch.randn((64, 1, H, d), generator=g, device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty((64, H, 1), device="cuda")
+    first = None
+    for space in (NONE, torch.randint(0, 256, (80 * 2 * 128 * d * 2,), dtype=torch.uint8, device="cuda"), None):
+        out.fill_(7.0)
+        c.attend_nodes_packed(nodes, q, out, lse, space=space)
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first)
+        for i in range(64):
+            k, v = (torch.cat([own[i][x, 0].double()] + [kv[(5 * i + j) % 80][x, 0] for j in range(16)]) for x in (0, 1))
+            assert_attention(out[i, :, 0], lse[i, 0], attention(q[i, :, 0], k, v), f"node {i}")
+    assert c.poll() == sva.OK
+    c.close()
