@@ -579,9 +579,9 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
           record_timeout(p, &abort_flag);
           break;
         }
-        // fault_mode 1 (test hook): withhold the V copy of the second tile,
-        // so the MMA issuer's bounded wait on it expires.
         if constexpr (kPacked) v_copy = packed ? v_copy & ~(1u << vs) : v_copy | 1u << vs;
+        // fault_mode 1 (test hook): withhold the V copy of the second tile (or the word
+        // that it may be unpacked), so the MMA issuer's bounded wait on it expires.
         if (!(p.fault_mode == 1 && j == 1)) {
           if (packed) {
             if constexpr (kPacked) mbar_arrive(&pack.v_go[vs]);
@@ -854,7 +854,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
           const typename PackRow<D>::Scales scales = row.scales;
           row.load_scales(then, r);
 #pragma unroll
-          for (int g = 0; g < D / kPackGroup; ++g) {
+          for (int g = 0; g < D / kPackGroup; ++g) {  // vectors of 32 elements
             const uint32_t sc = PackRow<D>::scale(scales, g);
             const uint32_t w[4] = {row.codes[g].x, row.codes[g].y, row.codes[g].z, row.codes[g].w};
 #pragma unroll

@@ -1926,6 +1926,8 @@ sva_status sva_cache_set_workspace(sva_cache* c, void* dev_buf, size_t bytes) {
     cudaGetLastError();
     return fail(SVA_ERR_INVALID_ARGUMENT, "workspace is not device memory of the cache's device");
   }
+  if (share_memory(dev_buf, ws_total_bytes(c), c->packed, c->packed_slots.size() * packed_slot_bytes(c->g, c->L)))
+    return fail(SVA_ERR_INVALID_ARGUMENT, "workspace shares memory with the packed slots");
   e = cudaMemset(dev_buf, 0, ws_counter_bytes(c));
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return cuda_fail(e, "zeroing the workspace counters");

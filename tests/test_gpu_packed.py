@@ -200,6 +200,11 @@ def test_refusals(sva_mod):
     host = torch.empty(sva.packed_bytes(c.g, 1) + 256, dtype=torch.uint8)
     at = (host.data_ptr() + 255) // 256 * 256
     assert lib.sva_cache_set_packed(c.handle, at, sva.packed_bytes(c.g, 1), 1) == bad
+    room = torch.empty(c.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    c.set_packed(room[-sva.packed_bytes(c.g, 1) // 256 * 256:], 1)
+    assert status(lambda: c.set_workspace(room)) == bad
+    c.set_packed(None)
+    c.set_workspace(room)
     c.set_packed(small, 2)
     assert c.bind_packed(0, 1, 0) == P and c.bind_packed(0, 2, 0) == P + 1
     c.release_packed(0, 1, 0)
