@@ -15,7 +15,9 @@
  * Around that: the input projection producing q, k, v (sva_qkv_project), the
  * RoPE + cache write (sva_rope_kv_write), a block-sparse form of the token
  * mask of Eq. 4 (sva_attend_nodes_sparse) and its token-level form on the
- * own chunk and on the history (sva_attend_nodes_masked).
+ * own chunk and on the history (sva_attend_nodes_masked); and for long histories
+ * states condensed by the attention they get (sva_cache_condense) or held in 4 bits
+ * (sva_cache_pack, sva_attend_nodes_packed).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -112,7 +114,8 @@ typedef struct {
  *                history states are always wholly visible
  *   n_ctx        number of history states read, 0..SVA_MAX_CTX
  *   ctx_slot     their cache slots (e.g. from sva_select_context +
- *                sva_cache_lookup), each of a chunk < `chunk`
+ *                sva_cache_lookup), each of a chunk < `chunk`; for
+ *                sva_attend_nodes_packed packed slots too
  *   ctx_visible  Eq. 4 at state granularity: 1 = mask 0 on that state's
  *                tokens, 0 = mask -inf (the state is skipped)           */
 typedef struct {
