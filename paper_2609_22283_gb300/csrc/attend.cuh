@@ -807,7 +807,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
     // What it costs the launch is its instructions (eleven and a store for eight elements),
     // which share the schedulers and the ALU with the softmax: 4680 queries over three
     // packed states of 12 heads 381 us, 312 with whole ones, 328 without the arithmetic.
-    // Eight such warps, with fewer registers for the softmax, the same to 3%; the work done
+    // Eight such warps, with fewer registers for the softmax, 2 to 9% slower; the work done
     // by the softmax warps between their steps 504 us (against 418 then).
     if constexpr (kPacked) {
       const int r = (int)threadIdx.x - kThreads;
