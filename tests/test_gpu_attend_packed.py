@@ -124,6 +124,11 @@ CASES = [
     dict(F=3, Hp=9, Wp=17, H=3, d=128, kinds="pwpp", nodes=2, causal=True),
     dict(F=3, Hp=9, Wp=17, H=3, d=64, kinds="pwpp", nodes=2, causal=True, hidden=(1,)),
     dict(F=1, Hp=7, Wp=30, H=2, d=128, kinds="ppp", hidden=(0, 1, 2)),
+    # full chunks whose query tiles see from a third to all of the own chunk: longest walks first
+    dict(F=3, Hp=30, Wp=52, H=2, d=128, kinds="p", causal=True),
+    dict(F=3, Hp=30, Wp=52, H=2, d=64, kinds="p", causal=True),
+    # no history at all
+    dict(F=1, Hp=9, Wp=15, H=2, d=128, kinds=""),
     # units split through the workspace: more of them than SMs, and a partial wave
     dict(F=3, Hp=20, Wp=26, H=12, d=128, kinds="pp", nodes=2),
     dict(F=3, Hp=20, Wp=26, H=14, d=64, kinds="pp", nodes=2),
