@@ -110,7 +110,7 @@ class PackedStream:
         c, self.device = self.cache, self.cache.buf.device
         c.set_workspace(torch.empty(c.workspace_bytes(), dtype=torch.uint8, device=self.device))
         if window > recent:
-            n = sequences * (window - recent)
+            n = sequences * (window - recent) + 1  # one to pack into before the oldest is let go
             c.set_packed(torch.empty(sva.packed_bytes(g, n), dtype=torch.uint8, device=self.device), n)
         self.window, self.recent, self.sequences = window, recent, sequences
         self.whole = {0: []}   # sequence -> [(chunk, slot)], oldest first
@@ -121,8 +121,8 @@ class PackedStream:
         return [s for _, s in self.packed[seq] + self.whole[seq]]
 
     def update(self, chunk, level, q, k, v, out, gamma_k=None, gamma_q=None, eps=1e-6, seq=0):
-        """One update of a chunk, arguments as Stream.update.  One that raises before its attention is launched leaves
-        no state behind, so that it can be made again."""
+        """One update of a chunk, arguments as Stream.update.  One that raises leaves the sequence's history as it was
+        and no state behind, so that it can be made again."""
         c, context = self.cache, self.context(seq)
         slot = c.bind(seq, chunk, level)
         try:
@@ -130,32 +130,35 @@ class PackedStream:
             rotated = torch.empty_like(out)
             c.rope_kv_write_headnorm(node, k, v, q, rotated, gamma_k, gamma_q, eps)
             c.attend_nodes_packed(node, rotated, out)
+            if level == 0:
+                self._keep(seq, chunk, slot)
         except BaseException:
             c.release(seq, chunk, level)
             raise
         if level != 0:
             c.release(seq, chunk, level)
-            return
-        self.whole[seq].append((chunk, slot))
-        if len(self.whole[seq]) > self.recent:
-            self._park(seq)
 
-    def _park(self, seq):
+    def _keep(self, seq, chunk, slot):
+        """The state joins the newest ones, and the oldest of these is packed if they are too many.  What may raise
+        comes before the lists change: the new packed slot is one to spare, the window's oldest is still held."""
         c, whole, packed = self.cache, self.whole[seq], self.packed[seq]
-        chunk, slot = whole[0]
+        if len(whole) < self.recent:
+            whole.append((chunk, slot))
+            return
+        old, at = (whole + [(chunk, slot)])[0]
         if self.window > self.recent:
-            if len(packed) == self.window - self.recent:
-                c.release_packed(seq, packed[0][0], 0)
-                del packed[0]
-            at = c.bind_packed(seq, chunk, 0)
+            to = c.bind_packed(seq, old, 0)
             try:
-                c.pack([slot], [at])
+                c.pack([at], [to])
             except BaseException:
-                c.release_packed(seq, chunk, 0)
+                c.release_packed(seq, old, 0)
                 raise
-            packed.append((chunk, at))
-        c.release(seq, chunk, 0)
+            packed.append((old, to))
+            if len(packed) > self.window - self.recent:
+                c.release_packed(seq, packed.pop(0)[0], 0)
+        whole.append((chunk, slot))
         del whole[0]
+        c.release(seq, old, 0)
 
     def fork(self, seq, new):
         """A new sequence `new` with the history of `seq`."""
