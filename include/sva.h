@@ -485,9 +485,10 @@ sva_status sva_attend_nodes_packed(sva_cache* c, const sva_node* nodes, int32_t 
                                    void* out, float* lse, float scale, const sva_attn_mask* mask,
                                    void* space, size_t space_bytes, sva_stream s);
 
-/* Bytes of space with which sva_attend_nodes_packed takes the least time for these nodes: 0 where
- * that is without one, where no visible context is packed, or where the call would be refused
- * for its nodes.  Masks are not counted.  Host-side only. */
+/* Bytes of space with which sva_attend_nodes_packed is estimated to take the least time for these
+ * nodes and the workspace that is attached: 0 where that is without one, where no visible context
+ * is packed, or where the call would be refused for its nodes or the current device.  Masks are
+ * not counted.  Host-side only. */
 size_t sva_attend_packed_space(const sva_cache* c, const sva_node* nodes, int32_t n_nodes);
 
 /* Copies n states in one launch: from src_slot[i] of `from` to dst_slot[i] of `to`, which may

@@ -1108,23 +1108,68 @@ sva_status check_space(const sva_cache* c, const Space& space, size_t need, cons
   return SVA_OK;
 }
 
+// What the plan of a launch goes by: its work units and the key tiles they walk.
+struct LaunchShape {
+  long long units = 0;
+  int min_tiles = 0, max_tiles = 0;
+  bool qp_major = false;
+};
+
+LaunchShape shape_of(const sva_cache* c, const sva::AttnNode* nodes, int n_nodes) {
+  const sva_geometry& g = c->g;
+  const int nt_slot = c->L.Tpad / sva::kTile;
+  LaunchShape r;
+  r.units = (long long)g.num_heads * n_nodes * ((nt_slot + 1) / 2);
+  r.min_tiles = 1 << 30;
+  long long kv_rows = 0;
+  bool fc = false;
+  for (int i = 0; i < n_nodes; ++i) {
+    r.min_tiles = std::min(r.min_tiles, key_tiles_walked(c, nodes[i], nt_slot));
+    r.max_tiles = std::max(r.max_tiles, nodes[i].n_kv * nt_slot);
+    kv_rows += 2LL * nodes[i].n_kv * g.num_heads * c->L.Tpad;
+    fc = fc || nodes[i].frame_causal;
+  }
+  // Pair-major order costs the L2 reuse of a head's K/V by the CTAs that run
+  // together, so it is taken where the pairs differ by more than a quarter and
+  // the launch's K/V (every node's slots, 64 MB of the 129 MB L2) stay in L2
+  // whatever the order.  First chunk of 4680 tokens, 12 heads: 13 to 37 key
+  // tiles a pair, 103 us head-major with the last wave split, 87 us so.
+  r.qp_major = fc && (r.max_tiles - r.min_tiles) * 4 > r.max_tiles && kv_rows * g.head_dim * 2 <= (64LL << 20);
+  return r;
+}
+
 // Is it faster to unpack a launch's packed states once, before the attention, than in each
-// of its work units?  Estimated in microseconds from measured launches (152 SMs, 64 to 4680
-// tokens, 1 to 40 heads, 1 to 16 packed states):
-//   - by the units: a packed key tile takes a CTA about 0.43 more (d = 64: 0.15), for the
-//     walks of the CTA that has most of them;
+// of its work units?  Estimated in microseconds from measured launches (152 SMs, 128 to 4680
+// tokens, 2 to 80 heads, 1 to 16 packed states, with a workspace and without):
+//   - by the units: a packed key tile takes a CTA about 0.43 more at d = 128; at d = 64 0.20
+//     with the states in L2 and 0.40 with them in HBM, of which 0.35 loses least.  Counted
+//     along the plan's waves: the whole ones of unsplit units, then those of the split ones.
+//     (Nodes that see fewer packed states than others make shorter units; the mean fills
+//     the waves, and no launch is shorter than its longest CTA.)
 //   - before them: a launch, the states' packed and whole bytes at 8.5 TB/s (the whole ones
 //     stay in L2 for the most part), and what is beyond 64 MB of them read back from HBM.
-// 4680 tokens of 12 heads, three states: 381 us and 329; 320 tokens of 40 heads, sixteen
-// states: 84 and 95; 320 of 12, four: 16.7 and 18.4; 2 x 2160 of 16 x 64, four: 195 and 178.
-bool unpacks_first(const sva_cache* c, const sva::AttnNode* nodes, int n_nodes, const PackedReads& r) {
+// By the units and unpacked first: 4680 tokens of 12 heads, three states 383 us and 330; 320 of
+// 40, sixteen 84 and 95; 320 of 12, eight 21.7 and 23.0, without a workspace 51.2 and 46.6; 640 of
+// 26, eight 73.4 and 76.0; 2 x 2160 of 16 x 64, four 195 and 179.  Over 252 such launches, in L2
+// and after a flush, the way taken was more than 3% behind the other one in 28 of 504 (10% in three).
+bool unpacks_first(const sva_cache* c, const sva::AttnNode* nodes, int n_nodes, const PackedReads& r,
+                   const LaunchShape& shape, const LaunchPlan& plan) {
   const sva_geometry& g = c->g;
-  const double sms = c->num_sms, nt = c->L.Tpad / sva::kTile, pairs = (c->L.Tpad / sva::kTile + 1) / 2;
-  const double units = (double)n_nodes * g.num_heads * pairs, walks = (double)r.refs * g.num_heads * pairs * nt;
-  const double ctas = std::min(sms, units * std::min<double>(sva::kMaxClusterSplit, std::max(1.0, std::floor(sms / units))));
+  const int nt = c->L.Tpad / sva::kTile;
+  const long long sms = c->num_sms;
+  int most = 0;
+  for (int i = 0; i < n_nodes; ++i) {
+    int seen = 0;
+    for (int k = 1; k < nodes[i].n_kv; ++k) seen += nodes[i].slot[k] >= SVA_PACKED;
+    most = std::max(most, seen);
+  }
+  const double mean = (double)r.refs * nt / n_nodes;  // packed tiles of a unit
+  const long long rest = ((shape.units - plan.n_full) * plan.n_split + sms - 1) / sms;
+  const double walks = std::max((double)(plan.n_full / sms) * mean + (double)rest * mean / plan.n_split,
+                                (double)most * nt / (plan.n_full > 0 ? 1 : plan.n_split));
   const double whole = (double)r.n * slot_stride(c), packed = (double)r.n * packed_slot_bytes(g, c->L);
-  const double by_units = walks / ctas * (g.head_dim == 128 ? 0.43 : 0.15);
-  return by_units > 2.0 + (whole + packed) / 8.5e6 + std::max(0.0, whole - 64e6) / 6.7e6;
+  return walks * (g.head_dim == 128 ? 0.43 : 0.35) >
+         2.0 + (whole + packed) / 8.5e6 + std::max(0.0, whole - 64e6) / 6.7e6;
 }
 
 // Where the key-range split partials of an attention launch go.
@@ -1179,11 +1224,10 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
   // The split plan.  The static scratch takes the plan a full caller
   // workspace would get, so both entry points compute the same result, within
   // a limit of its own (below).
-  int min_tiles = 1 << 30;
-  for (int i = 0; i < n_nodes; ++i)
-    min_tiles = std::min(min_tiles, key_tiles_walked(c, p.nodes[i], p.nt_slot));
+  const LaunchShape shape = shape_of(c, p.nodes, n_nodes);
+  const long long units = shape.units;
+  const int min_tiles = shape.min_tiles;
   p.n_qp = (p.n_qt + 1) / 2;
-  const long long units = (long long)g.num_heads * n_nodes * p.n_qp;
   long long cap = (scratch == Scratch::kStatic || c->ws != nullptr) ? ws_items(c) : 0;
   // A launch with token masks scans them first for the key tiles they leave
   // anything of, when a workspace can take the result and the launch is long
@@ -1196,24 +1240,8 @@ sva_status attend(sva_cache* c, const sva_node* nodes, int32_t n_nodes, const vo
     cap -= (long long)((scan_bytes + ws_item_bytes(c) - 1) / ws_item_bytes(c));
   }
   LaunchPlan plan;
-  // Pair-major order costs the L2 reuse of a head's K/V by the CTAs that run
-  // together, so it is taken where the pairs differ by more than a quarter and
-  // the launch's K/V (every node's slots, 64 MB of the 129 MB L2) stay in L2
-  // whatever the order.  First chunk of 4680 tokens, 12 heads: 13 to 37 key
-  // tiles a pair, 103 us head-major with the last wave split, 87 us so.
-  int max_tiles = 0;
-  long long kv_rows = 0;
-  for (int i = 0; i < n_nodes; ++i) {
-    max_tiles = std::max(max_tiles, p.nodes[i].n_kv * p.nt_slot);
-    kv_rows += 2LL * p.nodes[i].n_kv * g.num_heads * c->L.Tpad;
-  }
-  bool fc = false;
-  for (int i = 0; i < n_nodes; ++i) fc = fc || p.nodes[i].frame_causal;
-  p.qp_major = fc && (max_tiles - min_tiles) * 4 > max_tiles &&
-                       kv_rows * g.head_dim * 2 <= (64LL << 20)
-                   ? 1
-                   : 0;
-  st = plan_launch(c, units, min_tiles, max_tiles, p.qp_major != 0, cap, &plan);
+  p.qp_major = shape.qp_major ? 1 : 0;
+  st = plan_launch(c, units, min_tiles, shape.max_tiles, shape.qp_major, cap, &plan);
   if (st != SVA_OK) return st;
   const long long n_full = plan.n_full;
   const int n_split = plan.n_split;
@@ -1548,10 +1576,15 @@ size_t sva_attend_packed_space(const sva_cache* c, const sva_node* nodes, int32_
   if (c == nullptr || nodes == nullptr || n_nodes < 1 || n_nodes > SVA_MAX_NODES) return 0;
   static thread_local sva::AttnNode list[SVA_MAX_NODES];
   bool packed = false;
-  if (check_read(c, nodes, n_nodes, list, &packed) != SVA_OK || !packed) return 0;
+  if (check_device(c) != SVA_OK || check_read(c, nodes, n_nodes, list, &packed) != SVA_OK || !packed) return 0;
   static thread_local PackedReads reads;
   list_packed(c, list, n_nodes, false, &reads);
-  return unpacks_first(c, list, n_nodes, reads) ? (size_t)reads.n * slot_stride(c) : 0;
+  const LaunchShape shape = shape_of(c, list, n_nodes);
+  LaunchPlan plan;
+  if (plan_launch(c, shape.units, shape.min_tiles, shape.max_tiles, shape.qp_major, c->ws != nullptr ? ws_items(c) : 0,
+                  &plan) != SVA_OK)
+    return 0;
+  return unpacks_first(c, list, n_nodes, reads, shape, plan) ? (size_t)reads.n * slot_stride(c) : 0;
 }
 
 // Attention with the split scratch taken from the library's own device
