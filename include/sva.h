@@ -427,7 +427,8 @@ sva_status sva_cache_condense(sva_cache* c, const int32_t* src_slot, int32_t n_s
  * their largest magnitude a divided by 7 and rounded to 5 significant bits (halves up),
  * and each element x is held as the whole number nearest to x / s (halves away from
  * zero), -7 to 7.  It stands for that number times s, which is a bf16 number, so that
- * reading back rounds nothing, and packing what was read back gives the same again.  An
+ * reading back rounds nothing, and packing what was read back gives the same again (but for a
+ * from 2^-120 to below 2^-120 * (1 + 2^-6), where 7 s is below 2^-120 and gives zeros).  An
  * element is off by at most s / 2, about a / 14.  A group with a < 2^-120 holds zeros;
  * one with a NaN, an infinity or a >= 2^124 reads as NaN throughout.
  *
