@@ -1879,9 +1879,11 @@ sva_status sva_cache_copy(sva_cache* from, const int32_t* src_slot, sva_cache* t
     return fail(SVA_ERR_INVALID_ARGUMENT,
                 "the caches' states differ (heads, head dimension, frames, grid, rope_pairs or rope_theta)");
   const size_t slot_bytes = slot_stride(from), packed_bytes = packed_slot_bytes(a, from->L);
+  const size_t from_packed = from->packed_slots.size() * packed_bytes, to_packed = to->packed_slots.size() * packed_bytes;
   if (from != to && (share_memory(from->base, from->L.total, to->base, to->L.total) ||
-                     share_memory(from->packed, from->packed_slots.size() * packed_bytes, to->packed,
-                                  to->packed_slots.size() * packed_bytes)))
+                     share_memory(from->base, from->L.total, to->packed, to_packed) ||
+                     share_memory(from->packed, from_packed, to->base, to->L.total) ||
+                     share_memory(from->packed, from_packed, to->packed, to_packed)))
     return fail(SVA_ERR_INVALID_ARGUMENT, "the two caches share memory");
   const bool packed = src_slot[0] >= SVA_PACKED;
   sva::StateCopyParams p{};
