@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
         const int from = nd.slot[i / p.nt_slot];
         const bool packed = is_packed(from);
         const CUtensorMap* map = from >= kSpaceSlot ? &p.tmap_space : &p.tmap_kv;
-        const int slot = from & (kSpaceSlot - 1);
+        const int slot = packed ? 0 : from & (kSpaceSlot - 1);  // (a packed slot's rows may pass 2^31)
         const int t = i - (i / p.nt_slot) * p.nt_slot;
         const int row_k = ((slot * 2 + 0) * p.H + h) * p.Tpad + t * kTile;
         const int row_v = row_k + p.H * p.Tpad;
