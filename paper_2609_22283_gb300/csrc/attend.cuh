@@ -116,11 +116,11 @@ __device__ __forceinline__ uint32_t col_o(int b) {
 
 // 12 warps: warpgroup 0 = TMA producer (warp 0), MMA issuers (warps 1 and
 // 3), warp 2 (the block-sparse mask gather in the prologue, then idle);
-// warpgroups 1 and 2 = softmax.  The launch gives every thread kLaunchRegs
-// registers; warpgroup 0 then gives registers back (setmaxnreg.dec to
-// kRegsLow) and the softmax warpgroups take them (setmaxnreg.inc to
-// kRegsHigh).  The split must fit the launch's pool: 4*32*kRegsLow +
-// 8*32*kRegsHigh <= 384*kLaunchRegs, checked at launch.  At D = 64 a softmax
+// warpgroups 1 and 2 = softmax.  The launch gives every thread AttnRegs::kLaunch
+// registers; warpgroup 0 then gives registers back (setmaxnreg.dec to kLow)
+// and the softmax warpgroups take them (setmaxnreg.inc to kHigh).  The split
+// must fit the launch's pool: kPool <= kThreadsOf * kLaunch, and at the first launch
+// on a device the registers that the instance was built with.  At D = 64 a softmax
 // thread holds 128 scores and spills below 216 (88 + 208 was 3% slower).
 //
 // Instances that read packed slots have a fourth warpgroup (warps 12-15), which turns
@@ -1602,8 +1602,8 @@ __global__ void __launch_bounds__(AttnRegs<D, kPacked>::kThreadsOf, 1)
 
 }  // namespace
 
-// The kernel's instances are compiled in three units (attend_dense.cu,
-// attend_cluster.cu, attend_masked.cu), because in one the speed of the dense
+// The kernel's instances are compiled in four units (attend_dense.cu, attend_cluster.cu,
+// attend_masked.cu, attend_packed.cu), because in one the speed of the dense
 // instance was seen to change with the code of the others (a 4680-token layer
 // between 367 and 381 us for the same source of its own).  Why is not known:
 // after a change to this file, time the dense launches too, whichever instance
